@@ -266,6 +266,97 @@ int wkv_launch_shape(const wkv_options* opt, int* workgroups, int* threads);
 int wkv_probe_read(const void* src, size_t bytes, int workgroups, int threads, int nontemporal,
                    void* sink, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * The paged cache: every token of every sequence, uncompressed, in pages of a pool that the caller
+ * owns; a batch of sequences of any lengths, query heads that share K/V heads, and, if wanted, a
+ * sliding window with a few first tokens that stay visible, or eviction down to a budget by
+ * accumulated attention weight (the cumulative-score rule the paper cites as H2O, Section II),
+ * many entries at once.  There is no handle: a wkv_paged describes the caller's memory for one call.
+ *
+ * Sequence b holds L = lens[b] tokens in slots 0 .. L-1, those that the call brings included; its
+ * n new ones (one for wkv_paged_step) are the last.  The query in slot p attends over
+ *     { j <= p : window == 0, or j > p - window, or j < n_sink }
+ * with o_p = sum_j w_j v_j, w = softmax(q_p . k_j / sqrt(head_dim)); query head h uses K/V head
+ * h / (heads / kv_heads).  A row that sees nothing (or only logits of -inf) is all zeros.  What a
+ * row does not see has no effect on it, whatever it holds (infinities and NaNs included).
+ *
+ * Slot j lies in page table[b][j / page_size], at place j % page_size.  A table entry outside
+ * 0 .. n_pages-1 is a page that is not there (never given, or given back when the window had passed it): its
+ * slots are seen by no query, and rows that would go there are dropped.  Lengths are taken as at least 0 and
+ * at most max_pages * page_size (with scores: and score_stride).  A sequence of length 0 takes no
+ * part in a step: its output row is zeros, nothing is appended.
+ * Sequences may share pages that no call writes to (a common prompt).  Neither the pool nor the table is checked on
+ * the host: they are device memory.
+ */
+typedef struct wkv_paged {
+    void* k;                     /* DEVICE pools of n_pages pages, 16-byte aligned; the row of slot s,  */
+    void* v;                     /*   head h of page p starts at element p*page_stride + s*slot_stride + h*head_stride */
+    int64_t page_stride, slot_stride, head_stride;  /* in elements, not negative, each a multiple of 16 bytes */
+    const int32_t* table;        /* DEVICE, entry i of sequence b at table[b*table_stride + i]          */
+    int64_t table_stride;
+    const int32_t* lens;         /* DEVICE [batch]                                                      */
+    float* scores;               /* DEVICE, or NULL: accumulated attention weight of slot j for K/V head h of */
+    int64_t score_stride;        /*   sequence b at scores[(b*kv_heads + h)*score_stride + j]; a row ends within the last page */
+    int batch, heads, kv_heads;  /* heads is a multiple of kv_heads                                     */
+    int head_dim, dtype;         /* as wkv_options: {64,128,256} (fp32: {64,128})                       */
+    int page_size;               /* slots per page: a power of two, 16 .. 4096                          */
+    int n_pages, max_pages;      /* pages of the pool; table entries per sequence; max_pages*page_size <= 2^24 */
+    int window, n_sink;          /* 0, 0: every earlier token is seen; without a window n_sink counts in wkv_paged_evict only */
+    int reserved[4];             /* must be zero                                                        */
+} wkv_paged;
+
+/* Rows of a call, by token and head: DEVICE, 16-byte aligned; the row of token t and head h starts at element
+ * t*stride + h*head_stride.  Strides are multiples of 16 bytes and not negative (0: the same row for all; not for out). */
+typedef struct wkv_paged_rows {
+    const void* q;               /* [tokens][heads][head_dim]                                           */
+    const void* k;               /* [tokens][kv_heads][head_dim], or NULL (with v): appended already    */
+    const void* v;
+    void* out;                   /* as q                                                                */
+    int64_t q_stride, q_head_stride, k_stride, k_head_stride, v_stride, v_head_stride, out_stride, out_head_stride;
+} wkv_paged_rows;
+
+/* Bytes of DEVICE workspace (16-byte aligned) that wkv_paged_step, wkv_paged_evict and a wkv_paged_prefill of up to
+ * n_tokens tokens in all and max_new a sequence (0, 0: none) want for this cache; 0 if the description is invalid.
+ * The contents do not matter before a call, nor after it.  Calls that share a workspace must not overlap in time,
+ * recorded ones (HIP graphs) included.  Host-only arithmetic; pointers are not looked at, but for scores being NULL or not. */
+size_t wkv_paged_workspace_bytes(const wkv_paged* c, int n_tokens, int max_new);
+
+/*
+ * One token for every sequence, token b of the rows for sequence b.  Appends k and v to slot lens[b]-1, attends with q, and, with
+ * scores, adds to every slot the weights it got from the query heads of its group (the appended slot's sum starts with this).
+ * Asynchronous: returns after enqueueing on `stream`; nothing is allocated and nothing synchronised,
+ * so a step can be recorded into a HIP graph: lens, table and the rows are read when it runs.
+ * On error nothing is enqueued (WKV_EHIP: the launch itself failed).
+ */
+int wkv_paged_step(const wkv_paged* c, const wkv_paged_rows* rows, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * A chunk of new tokens for every sequence: tokens starts[b] .. starts[b+1]-1 of the rows are the last
+ * tokens of sequence b, in slots lens[b]-n .. lens[b]-1.  Appends k and v, attends, and with scores adds the weights, all queries' and heads' of the group together (appended slots' sums start with this).
+ *   starts  : DEVICE int32 [batch+1], not decreasing; rows behind starts[batch] are left as they are
+ *   n_tokens: tokens that the rows have; max_new: at least the longest chunk (longer ones are cut to it), at
+ *             most n_tokens.  A chunk longer than its sequence's lens[b]: its first rows have no slot; they see nothing.
+ * Asynchronous as wkv_paged_step.  How the work is shared out depends on the sizes (not on lens), and so do last bits;
+ * the same call gives the same bits every time.
+ */
+int wkv_paged_prefill(const wkv_paged* c, const wkv_paged_rows* rows, const int32_t* starts, int n_tokens, int max_new,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Cuts every sequence to `budget` slots, each K/V head by its own scores: of the L > budget slots the L - budget of lowest
+ * score that are neither among the first n_sink nor the newest recent_window leave (ties: the oldest first; a
+ * NaN counts as +inf), the others' rows, K and V, and sums move up in order, in the same pages.  Sequences of up to budget slots stay
+ * as they are, and so do those that miss one of the pages of their L slots.
+ *   new_lens   : DEVICE int32 [batch], receives the lengths; may be lens itself
+ *   new_scores : DEVICE, laid out as scores, receives the sums that are left and zeros up to L; may be scores itself
+ *   kept       : DEVICE int32 [batch][kv_heads][budget] or NULL, receives the slots where the rows that are left
+ *                were, then -1; all -1 for a sequence that misses a page
+ * Needs scores; 1 <= recent_window, n_sink + recent_window <= budget, and window == 0 (a window makes room by giving back pages).
+ * Pages of the L slots must belong to one sequence alone.  Asynchronous as wkv_paged_step.
+ */
+int wkv_paged_evict(const wkv_paged* c, int budget, int recent_window, int32_t* new_lens, float* new_scores, int32_t* kept,
+                    void* workspace, size_t workspace_bytes, void* stream);
+
 int wkv_version(void);
 
 #ifdef __cplusplus

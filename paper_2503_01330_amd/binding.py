@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -30,13 +31,27 @@ WKV_LOADS_AUTO, WKV_LOADS_CACHED, WKV_LOADS_STREAMING = 0, 1, 2
  WKV_EVICT_POS, WKV_EVICT_SLOT, WKV_STATUS) = range(11)
 
 EXPORTS = ("wkv_create", "wkv_create_ex", "wkv_step", "wkv_prefill", "wkv_prefill_noalloc", "wkv_state", "wkv_load", "wkv_destroy",
-           "wkv_last_error", "wkv_workspace_bytes", "wkv_step_bytes", "wkv_launch_shape", "wkv_probe_read", "wkv_version")
+           "wkv_last_error", "wkv_workspace_bytes", "wkv_step_bytes", "wkv_launch_shape", "wkv_probe_read", "wkv_paged_workspace_bytes",
+           "wkv_paged_step", "wkv_paged_prefill", "wkv_paged_evict", "wkv_version")
 
 
 class wkv_options(C.Structure):
     _fields_ = [(n, C.c_int) for n in ("batch", "heads", "head_dim", "budget", "recent_window",
                                         "dtype", "n_sink", "score_mode", "merge_mode",
                                         "log_capacity", "threads", "split", "streaming", "max_prompt", "replayable")] + [("reserved", C.c_int * 1)]
+
+
+class wkv_paged(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("k", "v")] + [(n, C.c_int64) for n in ("page_stride", "slot_stride", "head_stride")]
+                + [("table", C.c_void_p), ("table_stride", C.c_int64), ("lens", C.c_void_p), ("scores", C.c_void_p), ("score_stride", C.c_int64)]
+                + [(n, C.c_int) for n in ("batch", "heads", "kv_heads", "head_dim", "dtype", "page_size", "n_pages", "max_pages",
+                                          "window", "n_sink")] + [("reserved", C.c_int * 4)])
+
+
+class wkv_paged_rows(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("q", "k", "v", "out")]
+                + [(n, C.c_int64) for n in ("q_stride", "q_head_stride", "k_stride", "k_head_stride", "v_stride", "v_head_stride",
+                                            "out_stride", "out_head_stride")])
 
 
 class WkvError(RuntimeError):
@@ -66,6 +81,12 @@ _lib.wkv_step_bytes.restype = C.c_size_t
 _lib.wkv_step_bytes.argtypes = [C.POINTER(wkv_options)]
 
 
+_lib.wkv_paged_workspace_bytes.restype = C.c_size_t
+_lib.wkv_paged_workspace_bytes.argtypes = [C.POINTER(wkv_paged), C.c_int, C.c_int]
+_lib.wkv_paged_step.argtypes = [C.c_void_p] * 3 + [C.c_size_t, C.c_void_p]
+_lib.wkv_paged_prefill.argtypes = [C.c_void_p] * 3 + [C.c_int, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]
+_lib.wkv_paged_evict.argtypes = [C.c_void_p, C.c_int, C.c_int] + [C.c_void_p] * 4 + [C.c_size_t, C.c_void_p]
+_paged_step = _lib.wkv_paged_step
 _lib.wkv_probe_read.argtypes = [C.c_void_p, C.c_size_t, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p]
 
 
@@ -158,9 +179,13 @@ def wkv_launch_shape(opt: wkv_options):
 # The calling thread's current stream as an address.  torch.cuda.current_stream() makes an object of it first, 2.7 us, which is
 # more than the library takes to enqueue a small cache's step; torch has the address itself for its own launchers.
 if hasattr(torch._C, "_cuda_getCurrentRawStream") and hasattr(torch._C, "_cuda_getDevice"):
+    _current_device = torch._C._cuda_getDevice
+
     def _current_stream(_raw=torch._C._cuda_getCurrentRawStream, _device=torch._C._cuda_getDevice) -> int:
         return _raw(_device())
 else:
+    _current_device = torch.cuda.current_device
+
     def _current_stream() -> int:
         return torch.cuda.current_stream().cuda_stream
 
@@ -250,3 +275,121 @@ class Cache:
             self.close()
         except Exception:
             pass
+
+
+_pack_rows = struct.Struct("@4P8q").pack_into       # (fields of a ctypes structure, one by one, take 2 us)
+_TORCH_STORE = {torch.float32: WKV_FP32, torch.float16: WKV_FP16, torch.bfloat16: WKV_BF16}
+
+
+def _refuse(message):
+    raise WkvError(WKV_EINVAL, message)
+
+
+class PagedCache:
+    """A wkv_paged over torch tensors that the caller owns, and a workspace of its own.
+
+    k, v:   [n_pages, page_size, kv_heads, head_dim] on the GPU, any strides that are multiples of 16 bytes with the last one 1 (a
+            pool laid out [page][head][slot] is handed over transposed); float32, float16 or bfloat16
+    table:  int32 [batch, max_pages], lens: int32 [batch]
+    scores: float32 [batch, kv_heads, n], n within the last page, or None
+    The tensors are kept alive; what they hold is read when a call runs.  Calls on one object must not overlap in time
+    (the workspace is one); another object over the same tensors has its own.
+    """
+
+    def __init__(self, k, v, table, lens, heads, window=0, n_sink=0, scores=None, max_tokens=0, max_new=0):
+        if k.dim() != 4 or k.dtype not in _TORCH_STORE or v.shape != k.shape or v.dtype != k.dtype or v.stride() != k.stride():
+            _refuse("k and v: [n_pages, page_size, kv_heads, head_dim] of one type and layout")
+        if table.dim() != 2 or table.dtype != torch.int32 or lens.shape != table.shape[:1] or lens.dtype != torch.int32:
+            _refuse("table: int32 [batch, max_pages], lens: int32 [batch]")
+        if scores is not None and (scores.dtype != torch.float32 or scores.dim() != 3 or scores.shape[:2] != (table.shape[0], k.shape[2])):
+            _refuse("scores: float32 [batch, kv_heads, slots]")
+        for t in (k, table) + (() if scores is None else (scores,)):
+            if t.stride(-1) != 1 and t.shape[-1] != 1:
+                _refuse("the last dimension of pools, table and scores must be contiguous")
+        if not lens.is_contiguous() or (scores is not None and not scores.is_contiguous()):
+            _refuse("lens and scores must be contiguous")
+        self._tensors = (k, v, table, lens, scores)
+        if any(t is not None and t.device != k.device for t in self._tensors) or k.device.type != "cuda":
+            _refuse("pools, table, lens and scores must be on one GPU")
+        self.device, self.dtype, self.index = k.device, k.dtype, k.device.index
+        self.batch, self.heads, self.kv_heads, self.head_dim = table.shape[0], heads, k.shape[2], k.shape[3]
+        self.c = wkv_paged(k.data_ptr(), v.data_ptr(), *k.stride()[:3], table.data_ptr(), table.stride(0), lens.data_ptr(),
+                           scores.data_ptr() if scores is not None else None, scores.shape[2] if scores is not None else 0,
+                           self.batch, heads, self.kv_heads, self.head_dim, _TORCH_STORE[k.dtype], k.shape[1], k.shape[0], table.shape[1],
+                           window, n_sink)
+        self.rows = wkv_paged_rows()
+        self._ref, self._rows_ref = C.addressof(self.c), C.addressof(self.rows)
+        self._row, self._row_new = (heads, self.head_dim), (self.kv_heads, self.head_dim)
+        self._kept = []
+        self._work = None
+        self._reserve(max_tokens, max_new)
+
+    def _reserve(self, n_tokens, max_new):
+        need = _lib.wkv_paged_workspace_bytes(C.byref(self.c), n_tokens, max_new)
+        if need == 0:
+            _refuse("no workspace for these sizes: " + wkv_last_error())
+        if self._work is None or self._work.numel() < need:
+            self._kept.append(self._work)               # (work on another stream may still be using it)
+            self._work = torch.empty(need, dtype=torch.uint8, device=self.device)
+        self._at, self._bytes = self._work.data_ptr(), self._work.numel()
+
+    def _fill(self, n, q, k, v, out):
+        """The rows of a call, n tokens."""
+        if (k is None) != (v is None):
+            _refuse("k and v: both, or both None")
+        x = []
+        for t, shape in ((q, self._row), (k, self._row_new), (v, self._row_new), (out, self._row)):
+            if t is None:
+                x += (0, 0, 0)
+                continue
+            if t.dtype is not self.dtype or t.shape != (n, *shape) or t.get_device() != self.index:
+                _refuse(f"rows of a call: {[n, *shape]} in the cache's type, on its GPU")
+            s, h, e = t.stride()
+            if e != 1:
+                _refuse("the elements of a row must be next to each other")
+            x += (t.data_ptr(), s, h)
+        _pack_rows(self.rows, 0, x[0], x[3], x[6], x[9], x[1], x[2], x[4], x[5], x[7], x[8], x[10], x[11])
+
+    def _stream(self, stream):
+        if _current_device() != self.index:
+            _refuse(f"the cache belongs to device {self.index}, which is not the current one")
+        return _current_stream() if stream is None else stream
+
+    def step(self, q, k_new, v_new, out, stream=None):
+        """One token for every sequence: q, out [batch, heads, head_dim]; k_new, v_new [batch, kv_heads, head_dim], or both None
+        (appended already).  Any strides that are multiples of 16 bytes.  lens counts the new tokens."""
+        stream = self._stream(stream)
+        self._fill(self.batch, q, k_new, v_new, out)
+        rc = _paged_step(self._ref, self._rows_ref, self._at, self._bytes, stream)
+        if rc:
+            _check(rc)
+
+    def prefill(self, q, k, v, out, starts, max_new, stream=None):
+        """A chunk of new tokens for every sequence, tokens starts[b] .. starts[b + 1] of q, out [n_tokens, heads, head_dim] and
+        k, v [n_tokens, kv_heads, head_dim] (or both None); starts: int32 [batch + 1] on the GPU; max_new: the longest chunk.  The workspace
+        grows here if it has to (max_tokens and max_new of the constructor reserve it)."""
+        stream = self._stream(stream)
+        n = q.shape[0]
+        self._fill(n, q, k, v, out)
+        if starts.dtype != torch.int32 or starts.shape != (self.batch + 1,) or not starts.is_contiguous() or starts.get_device() != self.index:
+            _refuse("starts: int32 [batch + 1] on the cache's GPU")
+        if not 1 <= max_new <= n:
+            _refuse(f"1 <= max_new <= n_tokens is wanted: {max_new}, {n}")
+        self._reserve(n, max_new)
+        _check(_lib.wkv_paged_prefill(self._ref, self._rows_ref, starts.data_ptr(), n, max_new, self._at, self._bytes, stream))
+
+    def evict(self, budget, recent_window, new_lens, new_scores, kept=None, stream=None):
+        """Cuts every sequence to `budget` slots: new_lens int32 [batch], new_scores like scores, kept int32 [batch, kv_heads, budget].
+        new_lens and new_scores may be lens and scores themselves."""
+        stream = self._stream(stream)
+        scores = self._tensors[4]
+        for t, like, what in ((new_lens, self._tensors[3], "new_lens"), (new_scores, scores, "new_scores")):
+            if like is None:
+                _refuse("eviction needs scores")
+            if t.dtype != like.dtype or t.shape != like.shape or not t.is_contiguous() or t.device != self.device:
+                _refuse(f"{what} must be like what it replaces")
+        if kept is not None and (kept.dtype != torch.int32 or tuple(kept.shape) != (self.batch, self.kv_heads, budget)
+                                 or not kept.is_contiguous() or kept.device != self.device):
+            _refuse("kept: int32 [batch, kv_heads, budget]")
+        _check(_lib.wkv_paged_evict(self._ref, budget, recent_window, new_lens.data_ptr(), new_scores.data_ptr(),
+                                    kept.data_ptr() if kept is not None else None, self._at, self._bytes, stream))

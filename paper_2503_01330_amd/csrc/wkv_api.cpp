@@ -334,6 +334,8 @@ int prefill_reserve(wkv_handle* h, int tokens)
 
 }  // namespace
 
+int wkv_set_error(int code, const char* message) { return fail(code, "%s", message); }
+
 extern "C" {
 
 const char* wkv_last_error(void) { return g_err.c_str(); }

@@ -103,6 +103,56 @@ hipError_t wkv_launch_place_rows(const WkvCache& c, int what, int row_bytes, int
 hipError_t wkv_launch_place_items(const WkvCache& c, int unit0, int units, int len, const double* sums, const int32_t* pos,
                                   hipStream_t stream);
 
+// ---- the paged cache (wkv_paged.hip, wkv_evict.hip; wkv_paged_api.cpp checks the arguments)
+//
+// The cache of wkv.h's wkv_paged, strides in bytes.
+struct WkvPages {
+    char* k;
+    char* v;
+    int64_t page_bytes, slot_bytes, head_bytes;
+    const int32_t* table;
+    int64_t table_stride;
+    const int32_t* lens;
+    float* scores;
+    int64_t score_stride;
+    int batch, kv_heads, group;      // query heads per K/V head
+    int page_shift, n_pages, max_pages, max_slots, window, n_sink;
+};
+
+// One call of wkv_paged_step (starts null, max_new 1: a row per sequence) or wkv_paged_prefill.
+struct WkvPagedCall {
+    WkvPages c;
+    const char* q;
+    const char* k_new;               // null: appended already
+    const char* v_new;
+    char* out;
+    int64_t q_bytes, k_bytes, v_bytes, out_bytes;                 // from one token to the next
+    int64_t q_head, k_head, v_head, out_head;                     // from one head to the next
+    const int32_t* starts;
+    int n_tokens, max_new;
+    float scale;                     // log2(e) / sqrt(head_dim)
+    // workspace
+    int tiles, splits;               // row tiles of 16 per unit (sequence, K/V head); parts that a tile's keys are cut into at most
+    float* part;                     // [unit][tile][split][16][head_dim] sums of weight . v, when splits > 1
+    float* ml;                       // [unit][tile][split][2][16] reference (log2) and sum of the weights
+    float* logits;                   // [unit][group][logit_stride] q . k of a step whose weights are summed, or null
+    int64_t logit_stride;
+    float* lse;                      // [n_tokens][heads] log2 of the sum of exp(logit), of a prefill whose weights are summed, or null
+};
+
+hipError_t wkv_launch_paged_append(const WkvPagedCall& a, int dtype, int head_dim, hipStream_t stream);
+hipError_t wkv_launch_paged_attend(const WkvPagedCall& a, int dtype, int head_dim, hipStream_t stream);
+hipError_t wkv_launch_paged_sums(const WkvPagedCall& a, int dtype, int head_dim, hipStream_t stream);
+// How many parts wkv_launch_paged_attend should cut a tile's keys into.
+int wkv_paged_splits(int64_t tiles_in_all, int64_t most_keys, int dtype, int head_dim);
+
+// plan: [batch][2] lengths before and after; list: [unit][budget] slots that are left, ascending
+hipError_t wkv_launch_paged_evict(const WkvPages& c, int row_bytes, int budget, int recent, int32_t* new_lens, float* new_scores,
+                                  int32_t* kept, int32_t* plan, int32_t* list, hipStream_t stream);
+
+// The calling thread's error message, for the host files beside wkv_api.cpp; returns code.
+int wkv_set_error(int code, const char* message);
+
 // ---- measurement aid (wkv_probe.hip): `workgroups` x `threads` read `bytes` of device memory,
 // each workgroup its own contiguous share, and do nothing else.
 hipError_t wkv_launch_probe_read(const void* src, size_t bytes, int workgroups, int threads, bool nontemporal,
