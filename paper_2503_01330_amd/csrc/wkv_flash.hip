@@ -1,0 +1,378 @@
+// Attention of many new tokens over the paged cache (wkv_paged_prefill in include/wkv.h), 16-bit formats.
+//
+// A workgroup of four waves takes 128 rows of a unit (row r: token r / group, head r % group) and goes over the keys that they see, or
+// a part of them, in blocks of 64 (32 with wide heads).  K and V of a block travel from their pages straight into LDS, the next block's
+// while one is used.  A wave has 32 rows: S^T = K Q^T on the 32 x 32 x 16 instruction, whose result holds in a lane four consecutive keys
+// of one row at a time, as O^T = V^T P^T takes them for its second operand: weights stay in their lane.  The values' operand, eight keys
+// of one element, is read from LDS transposed.  A softmax with a running reference: the sums are scaled down only where a logit
+// exceeds the reference by more than 8 octaves.
+#include "../../include/wkv.h"
+#include "wkv_internal.h"
+#include "wkv_device.h"
+#include "wkv_paged_device.h"
+
+#include <type_traits>
+
+namespace {
+
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+
+constexpr int WAVES = 4, THREADS = 64 * WAVES, WAVE_ROWS = 32, TILE_ROWS = WAVES * WAVE_ROWS;
+
+template <class TT> __device__ __forceinline__ f32x16_t mfma32(u32x4_t a, u32x4_t b, f32x16_t c)
+{
+    if constexpr (__is_same(TT, TF16))
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+
+// What the values of keys that no row sees are taken from: whatever those hold, a weight of 0 times it has to be 0.
+__device__ __attribute__((aligned(16))) uint32_t zero_row[4];
+
+// 16 bytes of every lane from base + off (or from its own address) to 1 KiB of LDS, lane after lane.  Written out because the compiler
+// makes reads of LDS wait for all such loads that are under way.  They have no result in registers, and arrive() below waits for them.
+// (Nothing else here uses m0.)  LDS is addressed by number.
+template <class X> __device__ __forceinline__ const __attribute__((address_space(3))) X* lds_ptr(uint32_t at)
+{
+    return (const __attribute__((address_space(3))) X*)(uintptr_t)at;
+}
+__device__ __forceinline__ void load_lds(const char* base, uint32_t off, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
+}
+__device__ __forceinline__ void load_lds(const char* from, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
+}
+
+template <int D> struct Block {
+    static constexpr int BK = D > 128 ? 32 : 64;           // keys
+    static constexpr int CHUNKS = D / 8;                   // 16-byte pieces of a row
+    static constexpr int RPL = 64 / CHUNKS;                // rows of a load (64 lanes, 16 bytes each)
+    static constexpr int LOADS = BK / RPL / WAVES;         // loads of a wave
+    static constexpr int BYTES = BK * D * 2;
+    // The pieces of a row are stored at place (piece ^ turn): lanes that read the same piece of consecutive keys (K), or
+    // 4 keys' pairs of pieces (V), then touch different banks.
+    static constexpr int turn_k(int key) { return D == 64 ? key & 7 : key & 15; }
+    static constexpr int turn_v(int key) { return D == 64 ? (key & 3) << 1 : (key & 7) << 1; }
+};
+
+template <class TT, int D>
+__global__ __launch_bounds__(THREADS, D > 128 ? 1 : 2)
+void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
+{
+    using B = Block<D>;
+    constexpr int BK = B::BK, NB = BK / 32, KS = D / 16, DB = D / 32;
+    __shared__ __attribute__((aligned(1024))) char s_kv[4 * B::BYTES];
+    const uint32_t s_k0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)s_kv, s_v0 = s_k0 + B::BYTES;
+    const uint32_t s_k1 = s_k0 + 2 * B::BYTES, s_v1 = s_k0 + 3 * B::BYTES;
+
+    // Workgroups are dealt to the chip's eight partitions in turn: with spread, all of a unit's go to one of them, whose cache then
+    // holds the unit's K and V.  Tiles far into the sequence, which have the most keys, come first.
+    int id = blockIdx.x, unit;
+    const int per_unit = tiles * a.splits;
+    if (spread) {
+        const int x = id & 7;
+        id >>= 3;
+        unit = id / per_unit * 8 + x;
+        id = id % per_unit;
+    } else {
+        unit = id / per_unit;
+        id = id % per_unit;
+    }
+    const int part = id % a.splits, tile = tiles - 1 - id / a.splits;
+    Tile t;
+    if (!unit_of(a, unit, tile * TILE_ROWS, t)) return;
+    const WkvPages& c = a.c;
+    const int group = c.group;
+    const int r0 = tile * TILE_ROWS, r1 = min(t.rows, r0 + TILE_ROWS);
+    const int t_lo = t.pos0 + r0 / group, t_hi = t.pos0 + (r1 - 1) / group;       // positions of the tile's tokens
+    const Span sp = span(a, t_lo, t_hi);
+    if (part >= sp.parts) return;
+    const int begin = part * sp.per, end = min(sp.blocks, begin + sp.per);
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 31, half = lane >> 5;
+    const int window = c.window > 0 ? c.window : 0x40000000;
+    const int in_page = (1 << c.page_shift) - 1;
+
+    // the lane's row, and the positions of the wave's
+    const int w0 = r0 + wave * WAVE_ROWS;
+    const int row = w0 + col;
+    const int token = min(row, r1 - 1) / group, head = t.h * group + min(row, r1 - 1) - token * group;
+    const int p_row = row < r1 ? t.pos0 + token : -1;
+    const int p_lo = t.pos0 + min(w0, r1 - 1) / group, p_hi = t.pos0 + (min(w0 + WAVE_ROWS, r1) - 1) / group;
+    u32x4_t q[KS];
+    {
+        const char* src = a.q + (t.q.row0 + token) * a.q_bytes + head * a.q_head + half * 16;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) q[s] = *reinterpret_cast<const u32x4_t*>(src + s * 32);
+    }
+
+    const int32_t* table = c.table + t.b * c.table_stride;
+    auto slot_of = [&](int blk) { const int i = blk * BK; return __builtin_amdgcn_readfirstlane(i < sp.first ? i : i - sp.first + sp.lo); };
+    constexpr int NG = BK / 16;
+    // pages of a block's stretches of 16 slots, as the table says
+    auto entries = [&](int pos, int (&e)[NG]) {
+#pragma unroll
+        for (int i = 0; i < NG; ++i) e[i] = load_uniform(table + min((pos + i * 16) >> c.page_shift, c.max_pages - 1));
+    };
+    // -1 for what is none
+    auto known = [&](int pos, int (&e)[NG]) {
+#pragma unroll
+        for (int i = 0; i < NG; ++i) e[i] = (unsigned)e[i] < (unsigned)c.n_pages && pos + i * 16 < c.max_slots ? e[i] : -1;
+    };
+    auto all_there = [&](const int (&e)[NG]) {
+        bool x = true;
+#pragma unroll
+        for (int i = 0; i < NG; ++i) x &= e[i] >= 0;
+        return x;
+    };
+
+    const int lrow = lane / B::CHUNKS, lpiece = lane % B::CHUNKS;
+    const char* kh = c.k + t.h * c.head_bytes;
+    const char* vh = c.v + t.h * c.head_bytes;
+    auto load = [&](uint32_t kb, uint32_t vb, int pos, const int (&pages)[NG]) {
+        // every key is one that some row of the tile sees, or at least a finite one
+        const bool inside = all_there(pages) && pos + BK - 1 <= t_hi && (pos > t_lo - window || pos + BK <= c.n_sink);
+        const uint32_t down = (uint32_t)(lrow * (int)c.slot_bytes), kl = kb + wave * 1024, vl = vb + wave * 1024;
+        // load i: its first row, the lane's, the page (in narrow rows the waves' loads are of two stretches of 16 slots)
+        auto first = [&](int i) { return (i * WAVES + wave) * B::RPL; };
+        auto page_of = [&](int i) {
+            return WAVES * B::RPL > 16 ? (wave * B::RPL >= 16 ? pages[2 * i + 1] : pages[2 * i]) : pages[i * WAVES * B::RPL / 16];
+        };
+        if (inside) {
+#pragma unroll
+            for (int i = 0; i < B::LOADS; ++i) {
+                const int64_t at = page_of(i) * c.page_bytes + ((pos + first(i)) & in_page) * c.slot_bytes;
+                load_lds(kh + at, down + ((lpiece ^ B::turn_k(first(i) + lrow)) * 16), kl + i * (WAVES * 1024));
+                load_lds(vh + at, down + ((lpiece ^ B::turn_v(first(i) + lrow)) * 16), vl + i * (WAVES * 1024));
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < B::LOADS; ++i) {
+                const int page = page_of(i), in = first(i) + lrow, p = pos + in;
+                const int64_t at = max(page, 0) * c.page_bytes + ((pos + first(i)) & in_page) * c.slot_bytes;
+                const bool any = page >= 0 && p <= t_hi && (p > t_lo - window || p < c.n_sink);
+                const char* vs = vh + at + (down + ((lpiece ^ B::turn_v(in)) * 16));
+                load_lds(kh + at + (down + ((lpiece ^ B::turn_k(in)) * 16)), kl + i * (WAVES * 1024));
+                load_lds(any ? vs : reinterpret_cast<const char*>(zero_row), vl + i * (WAVES * 1024));
+            }
+        }
+    };
+
+    // Where the lane reads: K's piece 2 i + half of key col, V's piece of elements 32 i + (lane & 31) of the key of its four lanes; other
+    // keys and pieces are at fixed distances, but for the turn, which flips bits.
+    const uint32_t k_at = col * (D * 2) + ((half ^ B::turn_k(col)) << 4);
+    const int v_key = half * 4 + ((lane & 15) >> 2);
+    const uint32_t v_at = v_key * (D * 2) + (((((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) ^ B::turn_v(v_key)) << 4) + (lane & 1) * 8;
+
+    float ref = -INFINITY, l = 0.f;       // log2 of the weights' reference; the sum of the lane's weights
+    f32x16_t o[DB];
+#pragma unroll
+    for (int i = 0; i < DB; ++i)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
+
+    auto use = [&](uint32_t kb, uint32_t vb, int pos, const int (&pages)[NG]) {
+        if (pos > p_hi) return;                                            // (the wave's rows are all before it)
+        f32x16_t s[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            s[b] = f32x16_t{};
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+                const u32x4_t k = *lds_ptr<u32x4_t>((k_at ^ (i << 5)) + kb + b * 32 * (D * 2));
+                s[b] = mfma32<TT>(k, q[i], s[b]);
+            }
+        }
+        const bool full = all_there(pages) && pos + BK - 1 <= p_lo && (pos > p_hi - window || pos + BK <= c.n_sink);
+        if (!full) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const int p = pos + b * 32 + (j >> 2) * 8 + half * 4 + (j & 3);
+                    const bool seen = pages[b * 2 + (j >> 3)] >= 0 && p <= p_row && (p > p_row - window || p < c.n_sink);
+                    s[b][j] = seen ? s[b][j] : -INFINITY;
+                }
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) top = fmaxf(top, s[b][j]);
+        {
+            float x0, x1;
+            lane_pair<32>(top, x0, x1);
+            top = fmaxf(x0, x1) * a.scale;
+        }
+        if (__any(top > ref + 8.f)) {
+            const float now = fmaxf(ref, top);
+            const float f = ref == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref - now);
+            ref = now;
+            l *= f;
+#pragma unroll
+            for (int i = 0; i < DB; ++i)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) o[i][j] *= f;
+        }
+        const float minus = -((ref == -INFINITY ? 0.f : ref) + BIAS<TT>);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                s[b][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][j], a.scale, minus));
+                l += s[b][j];
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {                                  // 16 keys each
+                // weights rounded to the format: an error of the size of the output's own rounding
+                u32x4_t p;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) p[w] = pack2<TT>(s[b][j * 8 + 2 * w], s[b][j * 8 + 2 * w + 1]);
+#pragma unroll
+                for (int i = 0; i < DB; ++i) {
+                    const uint32_t at = (v_at ^ (i << 6)) + vb + (b * 32 + j * 16) * (D * 2);
+                    const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)lds_ptr<s16x4_t>(at));
+                    const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)lds_ptr<s16x4_t>(at + 8 * (D * 2)));
+                    const u32x2_t lw = __builtin_bit_cast(u32x2_t, lo), hw = __builtin_bit_cast(u32x2_t, hi);
+                    const u32x4_t v = {lw.x, lw.y, hw.x, hw.y};
+                    o[i] = mfma32<TT>(v, p, o[i]);
+                }
+            }
+        }
+    };
+
+    // Every wave has waited for its own loads of a block when it comes to the barrier, and has read all of the block before: after it
+    // the block is whole, and the other buffer is free for the next.
+    auto arrive = [&] {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0x0F70);               // vmcnt(0), in a form that the compiler counts by
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    int pos = slot_of(begin), pages[NG], next = 0, after[NG];
+    if (begin < end) {
+        entries(pos, pages);
+        known(pos, pages);
+        load(s_k0, s_v0, pos, pages);
+        next = slot_of(min(begin + 1, end - 1));
+        entries(next, after);
+    }
+    auto round = [&](int blk, uint32_t k, uint32_t v, uint32_t k_next, uint32_t v_next) {
+        arrive();
+        known(next, after);
+        if (blk + 1 < end) load(k_next, v_next, next, after);
+        const int p = pos;
+        int e[NG];
+#pragma unroll
+        for (int i = 0; i < NG; ++i) { e[i] = pages[i]; pages[i] = after[i]; }
+        pos = next;
+        next = slot_of(min(blk + 2, end - 1));
+        entries(next, after);
+        use(k, v, p, e);
+    };
+    for (int blk = begin; blk < end; blk += 2) {
+        round(blk, s_k0, s_v0, s_k1, s_v1);
+        if (blk + 1 < end) round(blk + 1, s_k1, s_v1, s_k0, s_v0);
+    }
+
+    l = pair_sum<32>(l);
+    // A value that is not finite spoils the sums of rows that do not see it (0 x infinity).  They are finite otherwise; if one is not, the wave
+    // forms them anew, key by key: a lane has a row and half of its elements.
+    float z = 0.f;
+#pragma unroll
+    for (int i = 0; i < DB; ++i)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) z = __builtin_fmaf(o[i][j], 0.f, z);
+    const bool spoilt = __any(z != 0.f);                                   // (0 x infinity and 0 x NaN are NaN, which is no 0)
+    if (spoilt) {
+#pragma unroll
+        for (int i = 0; i < DB; ++i)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
+        const char* qr = a.q + (t.q.row0 + token) * a.q_bytes + head * a.q_head;
+        const float minus = -((ref == -INFINITY ? 0.f : ref) + BIAS<TT>);
+#pragma unroll 1
+        for (int blk = begin; blk < end; ++blk) {
+            const int p0 = slot_of(blk);
+#pragma unroll 1
+            for (int k = 0; k < BK; ++k) {
+                const int p = p0 + k;
+                if (p >= c.max_slots) break;
+                const int page = load_uniform(table + (p >> c.page_shift));
+                if ((unsigned)page >= (unsigned)c.n_pages) continue;
+                const int64_t at = page * c.page_bytes + (p & in_page) * c.slot_bytes + t.h * c.head_bytes;
+                float dot = 0.f;
+#pragma unroll 1
+                for (int e = half * (D / 2); e < (half + 1) * (D / 2); ++e) dot += load_elem<TT>(qr, e) * load_elem<TT>(c.k + at, e);
+                dot = pair_sum<32>(dot);
+                if (p <= p_row && (p > p_row - window || p < c.n_sink)) {
+                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(dot, a.scale, minus));
+#pragma unroll
+                    for (int i = 0; i < DB; ++i)
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) o[i][j] += w * load_elem<TT>(c.v + at, i * 32 + (j >> 2) * 8 + half * 4 + (j & 3));
+                }
+            }
+        }
+    }
+
+    const bool direct = sp.parts == 1, mine = row < r1;
+    if (direct) {
+        const float inv = l != 0.f ? 1.f / l : 0.f;
+        char* dst = a.out + (t.q.row0 + token) * a.out_bytes + head * a.out_head;
+#pragma unroll
+        for (int i = 0; i < DB; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; j += 2) {                               // elements 8 j .. 8 j + 15 of the 32: halves of a lane pair joined
+                uint32_t w[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    w[k] = pack2<TT>(mean<TT>(o[i][(j + (k >> 1)) * 4 + (k & 1) * 2], inv), mean<TT>(o[i][(j + (k >> 1)) * 4 + (k & 1) * 2 + 1], inv));
+                const uint2v_t x = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+                const uint2v_t y = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+                if (mine) *reinterpret_cast<u32x4_t*>(dst + (i * 32 + (j + half) * 8) * 2) = u32x4_t{x.x, y.x, x.y, y.y};
+            }
+    } else {
+        float* cell = a.part + ((((int64_t)unit * a.tiles + row / ROWS) * a.splits + part) * ROWS + row % ROWS) * D;
+        if (mine) {
+#pragma unroll
+            for (int i = 0; i < DB; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    *reinterpret_cast<f32x4_t*>(cell + i * 32 + j * 8 + half * 4) = f32x4_t{o[i][j * 4], o[i][j * 4 + 1], o[i][j * 4 + 2], o[i][j * 4 + 3]};
+        }
+    }
+    if (mine && half == 0) {
+        if (a.ml) {
+            float* ml = a.ml + (((int64_t)unit * a.tiles + row / ROWS) * a.splits + part) * 32 + row % ROWS;
+            ml[0] = ref;
+            ml[16] = l;
+        }
+        if (a.lse && direct)
+            a.lse[(int64_t)(t.q.row0 + token) * (c.kv_heads * group) + head] = ref == -INFINITY ? INFINITY : ref + BIAS<TT> + __builtin_amdgcn_logf(l);
+    }
+}
+
+}  // namespace
+
+hipError_t wkv_launch_paged_flash(const WkvPagedCall& a, int dtype, int head_dim, hipStream_t stream)
+{
+    const int units = a.c.batch * a.c.kv_heads, tiles = (a.tiles * ROWS + TILE_ROWS - 1) / TILE_ROWS;
+    const int spread = units % 8 == 0;
+    auto go = [&](auto t, auto d) {
+        using TT = decltype(t);
+        constexpr int D = decltype(d)::value;
+        hipLaunchKernelGGL((wkv_paged_flash_kernel<TT, D>), dim3((unsigned)((int64_t)units * tiles * a.splits)), dim3(THREADS), 0, stream, a, tiles, spread);
+        return hipGetLastError();
+    };
+    auto wide = [&](auto t) {
+        return head_dim == 64 ? go(t, std::integral_constant<int, 64>{}) : head_dim == 128 ? go(t, std::integral_constant<int, 128>{})
+                                                                                           : go(t, std::integral_constant<int, 256>{});
+    };
+    return dtype == WKV_FP16 ? wide(TF16{}) : wide(TBF16{});
+}

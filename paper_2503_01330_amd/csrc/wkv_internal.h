@@ -133,6 +133,8 @@ struct WkvPagedCall {
     float scale;                     // log2(e) / sqrt(head_dim)
     // workspace
     int tiles, splits;               // row tiles of 16 per unit (sequence, K/V head); parts that a tile's keys are cut into at most
+    bool many;                       // the kernel for many rows (wkv_flash.hip) and not the one for few
+    int tile_rows, block, least;     // that kernel's rows a tile, keys a block, blocks a part at least
     float* part;                     // [unit][tile][split][16][head_dim] sums of weight . v, when splits > 1
     float* ml;                       // [unit][tile][split][2][16] reference (log2) and sum of the weights
     float* logits;                   // [unit][group][logit_stride] q . k of a step whose weights are summed, or null
@@ -143,8 +145,10 @@ struct WkvPagedCall {
 hipError_t wkv_launch_paged_append(const WkvPagedCall& a, int dtype, int head_dim, hipStream_t stream);
 hipError_t wkv_launch_paged_attend(const WkvPagedCall& a, int dtype, int head_dim, hipStream_t stream);
 hipError_t wkv_launch_paged_sums(const WkvPagedCall& a, int dtype, int head_dim, hipStream_t stream);
-// How many parts wkv_launch_paged_attend should cut a tile's keys into.
-int wkv_paged_splits(int64_t tiles_in_all, int64_t most_keys, int dtype, int head_dim);
+hipError_t wkv_launch_paged_flash(const WkvPagedCall& a, int dtype, int head_dim, hipStream_t stream);
+// Which kernel a call of `rows` rows a unit at most takes, and into how many parts it cuts a tile's keys, of which there are
+// most_keys at most: fills many, tiles, splits, tile_rows, block and least.
+void wkv_paged_shape(WkvPagedCall& a, int64_t units, int64_t rows, int64_t most_keys, int dtype, int head_dim);
 
 // plan: [batch][2] lengths before and after; list: [unit][budget] slots that are left, ascending
 hipError_t wkv_launch_paged_evict(const WkvPages& c, int row_bytes, int budget, int recent, int32_t* new_lens, float* new_scores,

@@ -16,19 +16,14 @@
 #include "../../include/wkv.h"
 #include "wkv_internal.h"
 #include "wkv_device.h"
+#include "wkv_paged_device.h"
 
 #include <algorithm>
 #include <type_traits>
 
 namespace {
 
-typedef float f32x4_t __attribute__((ext_vector_type(4)));
-typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-
 constexpr int WAVES = 4, THREADS = 64 * WAVES;
-constexpr int ROWS = 16;
 
 // How a format's rows are cut up for the matrix instructions.
 template <class TT, int D> struct Shape {
@@ -43,15 +38,6 @@ template <class TT, int D> struct Shape {
     static constexpr int NH = D / (16 * VE);               // such pieces of a row
     static constexpr int VW = VE * TT::BYTES / 4;          // words of a piece
 };
-
-template <class TT> __device__ __forceinline__ f32x4_t mfma(u32x4_t a, u32x4_t b, f32x4_t c)
-{
-    if constexpr (__is_same(TT, TF16))
-        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
-    else
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
-}
-__device__ __forceinline__ f32x4_t mfma_f32(float a, float b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
 // The product over 16 dwords of a row (a lane's KL loads): 16-bit rows 8 elements a load and instruction, fp32 rows 4 a load.
 template <class TT, int KL> __device__ __forceinline__ f32x4_t dot_tile(const u32x4_t (&a)[KL], const u32x4_t (&b)[KL])
@@ -68,94 +54,6 @@ template <class TT, int KL> __device__ __forceinline__ f32x4_t dot_tile(const u3
         }
     }
     return s;
-}
-
-// Two floats to two 16-bit elements, nearest even.
-template <class TT> __device__ __forceinline__ uint32_t pack2(float lo, float hi)
-{
-    if constexpr (__is_same(TT, TF16)) {
-        const half2_t h = {(_Float16)lo, (_Float16)hi};
-        return __builtin_bit_cast(uint32_t, h);
-    } else {
-        const bf16x2_t h = {(__bf16)lo, (__bf16)hi};
-        return __builtin_bit_cast(uint32_t, h);
-    }
-}
-template <class TT> __device__ __forceinline__ void unpack2(uint32_t w, float& lo, float& hi)
-{
-    if constexpr (__is_same(TT, TF16)) {
-        const half2_t h = __builtin_bit_cast(half2_t, w);
-        lo = (float)h.x; hi = (float)h.y;
-    } else {
-        lo = __builtin_bit_cast(float, w << 16); hi = __builtin_bit_cast(float, w & 0xFFFF0000u);
-    }
-}
-
-// Weights are 2^(logit - reference): the sums of 16-bit and fp32 values up to the format's largest stay finite while the
-// weights' own sum does not exceed 1, so where values reach 2^128 every weight is times 2^-24 (a sequence has at most 2^24 slots).
-template <class TT> constexpr float BIAS = __is_same(TT, TF16) ? 0.f : 24.f;
-
-// A row's output from its sum of weight . v.  It is a mean of values, so roundings must not take it over the format's largest number.
-template <class TT> __device__ __forceinline__ float mean(float sum, float inv)
-{
-    constexpr float MOST = __is_same(TT, TF16) ? 65504.f : __is_same(TT, TBF16) ? 0x1.FEp127f : 0x1.FFFFFEp127f;
-    const float x = sum * inv;
-    return __builtin_isinf(sum) ? x : x > MOST ? MOST : x < -MOST ? -MOST : x;
-}
-
-// ---------------------------------------------------------------- what a sequence and a tile have to do
-// A load whose address is the same in all lanes, through the scalar cache: it is not counted with the vector loads, so nothing
-// in flight there has to arrive first.  Nothing writes what is read so (tables) while a kernel here runs.
-__device__ __forceinline__ int32_t load_uniform(const int32_t* p)
-{
-    return *(const __attribute__((address_space(4))) int32_t*)(uintptr_t)p;
-}
-
-struct Seq { int len, n, row0; };      // tokens held, new ones among them, row of the first of these
-
-__device__ __forceinline__ Seq sequence(const WkvPagedCall& a, int b)
-{
-    Seq s;
-    s.len = min(max(a.c.lens[b], 0), a.c.max_slots);
-    if (a.starts) {
-        const int lo = min(max(a.starts[b], 0), a.n_tokens), hi = min(max(a.starts[b + 1], lo), a.n_tokens);
-        s.row0 = lo;
-        s.n = min(hi - lo, a.max_new);
-    } else {
-        s.row0 = b;
-        s.n = 1;
-    }
-    return s;
-}
-
-// Keys in the order in which a tile goes over them: the first `first` slots, then those from `lo` on up to the tile's last position,
-// both multiples of 32, so that a block of keys is a block of slots.
-struct Span { int first, lo, blocks, parts, per; };
-
-template <int BK> __device__ __forceinline__ Span span(const WkvPagedCall& a, int p_lo, int p_hi)
-{
-    Span s;
-    s.lo = a.c.window > 0 ? max(0, p_lo - a.c.window + 1) & ~31 : 0;
-    s.first = min((min(a.c.n_sink, s.lo) + 31) & ~31, s.lo);
-    const int keys = p_hi < 0 ? 0 : s.first + p_hi + 1 - s.lo;
-    s.blocks = (keys + BK - 1) / BK;
-    // parts of at least a block a wave; every part has blocks
-    const int parts = max(1, min(a.splits, (s.blocks + WAVES - 1) / WAVES));
-    s.per = max(1, (s.blocks + parts - 1) / parts);
-    s.parts = max(1, (s.blocks + s.per - 1) / s.per);
-    return s;
-}
-
-struct Tile { int b, h, rows, pos0; Seq q; };    // rows of the unit; position of the first new token
-
-__device__ __forceinline__ bool tile_of(const WkvPagedCall& a, int unit, int tile, Tile& t)
-{
-    t.b = unit / a.c.kv_heads;
-    t.h = unit - t.b * a.c.kv_heads;
-    t.q = sequence(a, t.b);
-    t.rows = t.q.n * a.c.group;
-    t.pos0 = t.q.len - t.q.n;
-    return tile * ROWS < t.rows;
 }
 
 template <class TT, int D> struct Frag {
@@ -178,11 +76,11 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
     const int tile = id % a.tiles;
     const int unit = id / a.tiles;
     Tile t;
-    if (!tile_of(a, unit, tile, t)) return;
+    if (!unit_of(a, unit, tile * ROWS, t)) return;
     const int group = a.c.group;
     const int r0 = tile * ROWS, r1 = min(t.rows, r0 + ROWS);
     const int p_lo = t.pos0 + r0 / group, p_hi = t.pos0 + (r1 - 1) / group;
-    const Span sp = span<BK>(a, p_lo, p_hi);
+    const Span sp = span(a, p_lo, p_hi);
     if (part >= sp.parts) return;
     const int begin = part * sp.per, end = min(sp.blocks, begin + sp.per);
 
@@ -506,10 +404,12 @@ void wkv_paged_join_kernel(const WkvPagedCall a, int per_tile)
     const int cell = blockIdx.x / per_tile, piece = blockIdx.x - cell * per_tile;
     const int unit = cell / a.tiles, tile = cell - unit * a.tiles;
     Tile t;
-    if (!tile_of(a, unit, tile, t)) return;
+    if (!unit_of(a, unit, tile * ROWS, t)) return;
     const int group = a.c.group, r0 = tile * ROWS, r1 = min(t.rows, r0 + ROWS);
-    const int p_lo = t.pos0 + r0 / group, p_hi = t.pos0 + (r1 - 1) / group;
-    const Span sp = span<S::BK>(a, p_lo, p_hi);
+    // the keys were cut into parts for a tile of a.tile_rows rows
+    const int t0 = r0 & -a.tile_rows, t1 = min(t.rows, t0 + a.tile_rows);
+    const int p_lo = t.pos0 + t0 / group, p_hi = t.pos0 + (t1 - 1) / group;
+    const Span sp = span(a, p_lo, p_hi);
 
     const int row = threadIdx.x >> 4, lane = threadIdx.x & 15;
     if (piece == 0 && sp.parts > 1 && r0 + row < r1) {
@@ -588,7 +488,7 @@ void wkv_paged_sums_kernel(const WkvPagedCall a, int unit0, int per_unit)
     const WkvPages& c = a.c;
     const int unit = unit0 + blockIdx.x / per_unit;
     Tile t;
-    if (!tile_of(a, unit, 0, t)) return;
+    if (!unit_of(a, unit, 0, t)) return;
     const int window = c.window > 0 ? c.window : 0x40000000, group = c.group;
     const int in_page = (1 << c.page_shift) - 1;
 #pragma unroll 1
@@ -685,12 +585,15 @@ template <class F> hipError_t by_type(int dtype, int head_dim, F&& f)
 
 }  // namespace
 
-int wkv_paged_splits(int64_t tiles_in_all, int64_t most, int dtype, int head_dim)
+void wkv_paged_shape(WkvPagedCall& a, int64_t units, int64_t rows, int64_t most, int dtype, int head_dim)
 {
-    (void)head_dim;
-    const int64_t block = dtype == WKV_FP32 ? 16 : 32, rounds = (most + block * WAVES - 1) / (block * WAVES);
-    const int64_t want = (512 + tiles_in_all - 1) / tiles_in_all;
-    return (int)std::max<int64_t>(1, std::min<int64_t>({want, rounds, 64}));
+    a.tiles = (int)((rows + ROWS - 1) / ROWS);
+    a.many = dtype != WKV_FP32 && rows > 32;
+    a.tile_rows = a.many ? 128 : ROWS;
+    a.block = a.many ? (head_dim > 128 ? 32 : 64) : dtype == WKV_FP32 || head_dim > 128 ? 16 : 32;
+    a.least = WAVES;
+    const int64_t groups = units * ((rows + a.tile_rows - 1) / a.tile_rows), part = (int64_t)a.block * a.least;
+    a.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(512 + groups - 1) / groups, (most + part - 1) / part, 64}));
 }
 
 hipError_t wkv_launch_paged_append(const WkvPagedCall& a, int dtype, int head_dim, hipStream_t stream)
@@ -718,8 +621,13 @@ hipError_t wkv_launch_paged_attend(const WkvPagedCall& a, int dtype, int head_di
     return by_type(dtype, head_dim, [&](auto t, auto d) {
         using TT = decltype(t);
         constexpr int D = decltype(d)::value;
-        hipLaunchKernelGGL((wkv_paged_rows_kernel<TT, D>), dim3((unsigned)(units * a.tiles * a.splits)), dim3(THREADS), 0, stream, a);
-        hipError_t e = hipGetLastError();
+        hipError_t e;
+        if (a.many) {
+            e = wkv_launch_paged_flash(a, dtype, head_dim, stream);
+        } else {
+            hipLaunchKernelGGL((wkv_paged_rows_kernel<TT, D>), dim3((unsigned)(units * a.tiles * a.splits)), dim3(THREADS), 0, stream, a);
+            e = hipGetLastError();
+        }
         if (e == hipSuccess && (a.splits > 1 || a.logits)) {
             const int per_tile = a.logits ? (int)((a.c.max_slots + 64 + TALLY - 1) / TALLY) : 1;
             hipLaunchKernelGGL((wkv_paged_join_kernel<TT, D>), dim3((unsigned)(units * a.tiles * per_tile)), dim3(THREADS), 0, stream, a, per_tile);

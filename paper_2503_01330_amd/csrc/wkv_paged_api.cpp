@@ -77,7 +77,7 @@ WkvPages pages_of(const wkv_paged& p)
     return c;
 }
 
-// Most keys that a tile of rows of `new_tokens` tokens sees
+// Most keys that some query sees, or a tile of queries of up to new_tokens tokens
 int64_t most_keys(const WkvPages& c, int64_t new_tokens)
 {
     return c.window > 0 ? std::min<int64_t>(c.max_slots, (int64_t)c.window + c.n_sink + new_tokens + 64) : c.max_slots;
@@ -85,7 +85,7 @@ int64_t most_keys(const WkvPages& c, int64_t new_tokens)
 
 // Workspace of an attention call: each piece at a multiple of 256 bytes.
 struct Layout {
-    int tiles = 1, splits = 1;
+    WkvPagedCall shape = {};
     size_t part = 0, ml = 0, logits = 0, lse = 0, total = 0;
     int64_t logit_stride = 0;
 };
@@ -95,13 +95,13 @@ Layout layout(const wkv_paged& p, bool scores, int n_tokens, int max_new, bool s
     const WkvPages c = pages_of(p);
     const int64_t units = (int64_t)c.batch * c.kv_heads;
     Layout l;
-    l.tiles = (int)(((int64_t)max_new * c.group + 15) / 16);
-    const int64_t tile_tokens = std::min<int64_t>(max_new, 15 / c.group + 2);
-    l.splits = wkv_paged_splits(units * l.tiles, most_keys(c, tile_tokens), p.dtype, p.head_dim);
+    const int64_t rows = (int64_t)max_new * c.group;
+    wkv_paged_shape(l.shape, units, rows, most_keys(c, std::min(max_new, 128 / c.group + 2)), p.dtype, p.head_dim);
     auto take = [&](size_t bytes) { const size_t at = l.total; l.total += (bytes + 255) / 256 * 256; return at; };
-    const size_t cells = (size_t)units * l.tiles * l.splits;
-    if (l.splits > 1) l.part = take(cells * 16 * p.head_dim * sizeof(float));
-    if (l.splits > 1 || (scores && step)) l.ml = take(cells * 32 * sizeof(float));
+    const int splits = l.shape.splits;
+    const size_t cells = (size_t)units * l.shape.tiles * splits;
+    if (splits > 1) l.part = take(cells * 16 * p.head_dim * sizeof(float));
+    if (splits > 1 || (scores && step)) l.ml = take(cells * 32 * sizeof(float));
     if (scores && step) {
         l.logit_stride = (c.max_slots + 31) / 32 * 32;
         l.logits = take((size_t)units * c.group * l.logit_stride * sizeof(float));
@@ -143,23 +143,22 @@ int attend(const wkv_paged* p, const wkv_paged_rows* r, const int32_t* starts, i
     const Layout l = layout(*p, p->scores != nullptr, n_tokens, max_new, step);
     rc = check_work(workspace, workspace_bytes, l.total);
     if (rc != WKV_OK) return rc;
-    WkvPagedCall a = {};
+    WkvPagedCall a = l.shape;
     a.c = pages_of(*p);
     a.q = (const char*)r->q; a.k_new = (const char*)r->k; a.v_new = (const char*)r->v; a.out = (char*)r->out;
     a.q_bytes = r->q_stride * eb; a.k_bytes = r->k_stride * eb; a.v_bytes = r->v_stride * eb; a.out_bytes = r->out_stride * eb;
     a.q_head = r->q_head_stride * eb; a.k_head = r->k_head_stride * eb; a.v_head = r->v_head_stride * eb; a.out_head = r->out_head_stride * eb;
     a.starts = starts; a.n_tokens = n_tokens; a.max_new = max_new;
     a.scale = (float)(1.4426950408889634 / std::sqrt((double)p->head_dim));
-    a.tiles = l.tiles; a.splits = l.splits;
     char* w = (char*)workspace;
-    if (l.splits > 1) a.part = (float*)(w + l.part);
-    if (l.splits > 1 || (p->scores && step)) a.ml = (float*)(w + l.ml);
+    if (a.splits > 1) a.part = (float*)(w + l.part);
+    if (a.splits > 1 || (p->scores && step)) a.ml = (float*)(w + l.ml);
     if (p->scores && step) { a.logits = (float*)(w + l.logits); a.logit_stride = l.logit_stride; }
     if (p->scores && !step) a.lse = (float*)(w + l.lse);
     // a launch of 2^32 threads and more is not refused by the runtime: the count wraps
     const int64_t units = (int64_t)p->batch * p->kv_heads;
-    if (units * l.tiles * l.splits >= 1 << 24)
-        return fail(WKV_ESIZE, "%lld row tiles in %d parts: a launch holds fewer than 2^32 threads", (long long)(units * l.tiles), l.splits);
+    if (units * a.tiles * a.splits >= 1 << 24)
+        return fail(WKV_ESIZE, "%lld row tiles in %d parts: a launch holds fewer than 2^32 threads", (long long)(units * a.tiles), a.splits);
     hipError_t e = hipSuccess;
     if (!step && r->k) e = wkv_launch_paged_append(a, p->dtype, p->head_dim, stream);
     if (e == hipSuccess) e = wkv_launch_paged_attend(a, p->dtype, p->head_dim, stream);

@@ -1,0 +1,120 @@
+// Device code that the kernels of the paged cache share (wkv_paged.hip, wkv_flash.hip): matrix instructions by format, rounding
+// to 16 bits, and what a sequence, a tile of rows and a part of its keys are.  Each kernel file gets its own copy.
+#ifndef WKV_PAGED_DEVICE_H
+#define WKV_PAGED_DEVICE_H
+
+#include "wkv_device.h"
+#include "wkv_internal.h"
+
+namespace {
+
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+
+constexpr int ROWS = 16;            // rows of a tile, and of a cell of the workspace
+
+template <class TT> __device__ __forceinline__ f32x4_t mfma(u32x4_t a, u32x4_t b, f32x4_t c)
+{
+    if constexpr (__is_same(TT, TF16))
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4_t mfma_f32(float a, float b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
+
+// Two floats to two 16-bit elements, nearest even.
+template <class TT> __device__ __forceinline__ uint32_t pack2(float lo, float hi)
+{
+    if constexpr (__is_same(TT, TF16)) {
+        const half2_t h = {(_Float16)lo, (_Float16)hi};
+        return __builtin_bit_cast(uint32_t, h);
+    } else {
+        const bf16x2_t h = {(__bf16)lo, (__bf16)hi};
+        return __builtin_bit_cast(uint32_t, h);
+    }
+}
+template <class TT> __device__ __forceinline__ void unpack2(uint32_t w, float& lo, float& hi)
+{
+    if constexpr (__is_same(TT, TF16)) {
+        const half2_t h = __builtin_bit_cast(half2_t, w);
+        lo = (float)h.x; hi = (float)h.y;
+    } else {
+        lo = __builtin_bit_cast(float, w << 16); hi = __builtin_bit_cast(float, w & 0xFFFF0000u);
+    }
+}
+
+// Weights are 2^(logit - reference), the reference being a logit that none exceeds by more than 8: sums of values up to the format's
+// largest stay finite while the weights' own sum does not exceed 1, so where values reach 2^128 every weight is times 2^-32 (a
+// sequence has at most 2^24 slots).
+template <class TT> constexpr float BIAS = __is_same(TT, TF16) ? 0.f : 32.f;
+
+// A row's output from its sum of weight . v.  It is a mean of values, so roundings must not take it over the format's largest number.
+template <class TT> __device__ __forceinline__ float mean(float sum, float inv)
+{
+    constexpr float MOST = __is_same(TT, TF16) ? 65504.f : __is_same(TT, TBF16) ? 0x1.FEp127f : 0x1.FFFFFEp127f;
+    const float x = sum * inv;
+    return __builtin_isinf(sum) ? x : x > MOST ? MOST : x < -MOST ? -MOST : x;
+}
+
+// ---------------------------------------------------------------- what a sequence and a tile have to do
+// A load whose address is the same in all lanes, through the scalar cache: it is not counted with the vector loads, so nothing
+// in flight there has to arrive first.  Nothing writes what is read so (tables) while a kernel here runs.
+__device__ __forceinline__ int32_t load_uniform(const int32_t* p)
+{
+    return *(const __attribute__((address_space(4))) int32_t*)(uintptr_t)p;
+}
+
+struct Seq { int len, n, row0; };      // tokens held, new ones among them, row of the first of these
+
+__device__ __forceinline__ Seq sequence(const WkvPagedCall& a, int b)
+{
+    Seq s;
+    s.len = min(max(a.c.lens[b], 0), a.c.max_slots);
+    if (a.starts) {
+        const int lo = min(max(a.starts[b], 0), a.n_tokens), hi = min(max(a.starts[b + 1], lo), a.n_tokens);
+        s.row0 = lo;
+        s.n = min(hi - lo, a.max_new);
+    } else {
+        s.row0 = b;
+        s.n = 1;
+    }
+    return s;
+}
+
+// Keys in the order in which a tile goes over them: the first `first` slots, then those from `lo` on up to the tile's last position,
+// both multiples of a block of keys, so that a block is one of slots.
+struct Span { int first, lo, blocks, parts, per; };
+
+__device__ __forceinline__ Span span(const WkvPagedCall& a, int p_lo, int p_hi)
+{
+    Span s;
+    const int low = a.block - 1;                          // (a power of two)
+    s.lo = a.c.window > 0 ? max(0, p_lo - a.c.window + 1) & ~low : 0;
+    s.first = min((min(a.c.n_sink, s.lo) + low) & ~low, s.lo);
+    const int keys = p_hi < 0 ? 0 : s.first + p_hi + 1 - s.lo;
+    s.blocks = (keys + low) / a.block;
+    // parts of at least a.least blocks; every part has some
+    const int parts = max(1, min(a.splits, (s.blocks + a.least - 1) / a.least));
+    s.per = max(1, (s.blocks + parts - 1) / parts);
+    s.parts = max(1, (s.blocks + s.per - 1) / s.per);
+    return s;
+}
+
+struct Tile { int b, h, rows, pos0; Seq q; };    // rows of the unit; position of the first new token
+
+// The unit's sequence; whether it has the row.
+__device__ __forceinline__ bool unit_of(const WkvPagedCall& a, int unit, int row, Tile& t)
+{
+    t.b = unit / a.c.kv_heads;
+    t.h = unit - t.b * a.c.kv_heads;
+    t.q = sequence(a, t.b);
+    t.rows = t.q.n * a.c.group;
+    t.pos0 = t.q.len - t.q.n;
+    return row < t.rows;
+}
+
+}  // namespace
+
+#endif
