@@ -84,7 +84,7 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
     }
     const int part = id % a.splits, tile = tiles - 1 - id / a.splits;
     Tile t;
-    if (!unit_of(a, unit, tile * TILE_ROWS, t)) return;
+    if (!unit_of<false>(a, unit, tile * TILE_ROWS, t)) return;
     const WkvPages& c = a.c;
     const int group = c.group;
     const int r0 = tile * TILE_ROWS, r1 = min(t.rows, r0 + TILE_ROWS);

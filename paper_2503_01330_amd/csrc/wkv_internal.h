@@ -135,6 +135,7 @@ struct WkvPagedCall {
     int tiles, splits;               // row tiles of 16 per unit (sequence, K/V head); parts that a tile's keys are cut into at most
     bool many;                       // the kernel for many rows (wkv_flash.hip) and not the one for few
     int tile_rows, block, least;     // that kernel's rows a tile, keys a block, blocks a part at least
+    int order;                       // a step: workgroups take the longest sequences first
     float* part;                     // [unit][tile][split][16][head_dim] sums of weight . v, when splits > 1
     float* ml;                       // [unit][tile][split][2][16] reference (log2) and sum of the weights
     float* logits;                   // [unit][group][logit_stride] q . k of a step whose weights are summed, or null
@@ -146,6 +147,8 @@ hipError_t wkv_launch_paged_append(const WkvPagedCall& a, int dtype, int head_di
 hipError_t wkv_launch_paged_attend(const WkvPagedCall& a, int dtype, int head_dim, hipStream_t stream);
 hipError_t wkv_launch_paged_sums(const WkvPagedCall& a, int dtype, int head_dim, hipStream_t stream);
 hipError_t wkv_launch_paged_flash(const WkvPagedCall& a, int dtype, int head_dim, hipStream_t stream);
+// Most keys that a query sees, or the queries of new_tokens tokens next to each other.
+int64_t wkv_paged_most_keys(const WkvPages& c, int64_t new_tokens);
 // Which kernel a call of `rows` rows a unit at most takes, and into how many parts it cuts a tile's keys, of which there are
 // most_keys at most: fills many, tiles, splits, tile_rows, block and least.
 void wkv_paged_shape(WkvPagedCall& a, int64_t units, int64_t rows, int64_t most_keys, int dtype, int head_dim);

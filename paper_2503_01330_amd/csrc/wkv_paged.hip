@@ -8,7 +8,8 @@
 //                    S^T = K Q^T leaves in a lane 4 consecutive keys of one row, which is what the second product's operand
 //                    wants (O^T = V^T P^T), so the weights never leave their lane; the values' operand is a transposition of 16-bit
 //                    words within a lane.  The waves' sums are joined through LDS.
-//   wkv_paged_join   the parts of a tile joined; for a step whose weights are summed, the weights of every slot.
+//   wkv_paged_join   the parts of a row joined (join_few: of few parts).
+//   wkv_paged_tally  the weights of a step summed for every slot, from the logits that wkv_paged_rows left and the parts' sums.
 //   wkv_paged_sums   the weights of a prefill's rows summed for every slot, from the rows' log-sum-exps.
 //   wkv_paged_append new K and V rows into their pages (a step's rows go there inside wkv_paged_rows).
 //
@@ -62,105 +63,168 @@ template <class TT, int D> struct Frag {
     uint32_t v[S::VK][S::NH][S::VW];
 };
 
-template <class TT, int D>
-__global__ __launch_bounds__(THREADS, (D * TT::BYTES > 256) ? 1 : 2)
+// STEP: a row per sequence and head.  EARLY: of a step, where neither a window nor the order of the sequences decides where a wave
+// begins.  LOGITS: of a step, whose weights are summed: its logits are stored (with every block, so that waits can be counted).
+template <class TT, int D, bool STEP, bool EARLY, bool LOGITS>
+__global__ __launch_bounds__(THREADS, D * TT::BYTES > 256 ? 2 : 3)
 void wkv_paged_rows_kernel(const WkvPagedCall a)
 {
     using S = Shape<TT, D>;
     constexpr int BK = S::BK, NT = S::NT, KL = S::KL, VK = S::VK, VE = S::VE, NH = S::NH, VW = S::VW;
+    constexpr int PIECES = D * TT::BYTES / 16;
     __shared__ float s_m[WAVES][ROWS], s_l[WAVES][ROWS];
     __shared__ float s_o[WAVES][ROWS][16 * VE + 4];
+    __shared__ u32x4_t s_new[WAVES][2 * PIECES];
 
     int id = blockIdx.x;
     const int part = id % a.splits; id /= a.splits;
     const int tile = id % a.tiles;
-    const int unit = id / a.tiles;
-    Tile t;
-    if (!unit_of(a, unit, tile * ROWS, t)) return;
-    const int group = a.c.group;
-    const int r0 = tile * ROWS, r1 = min(t.rows, r0 + ROWS);
-    const int p_lo = t.pos0 + r0 / group, p_hi = t.pos0 + (r1 - 1) / group;
-    const Span sp = span(a, p_lo, p_hi);
-    if (part >= sp.parts) return;
-    const int begin = part * sp.per, end = min(sp.blocks, begin + sp.per);
-
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int col = lane & 15, g = lane >> 4;
+    int unit = id / a.tiles;
     const WkvPages& c = a.c;
-    const int window = c.window > 0 ? c.window : 0x40000000;
+    // Longest sequences first: what is left when the last workgroups have started is short then.
+    if (STEP && !EARLY && a.order) {
+        __shared__ __attribute__((aligned(16))) int s_len[THREADS];
+        __shared__ int s_mine;
+        const int place = unit / c.kv_heads, base = place / THREADS * THREADS, n = min(THREADS, c.batch - base);
+        const int len = (int)threadIdx.x < n ? c.lens[base + threadIdx.x] : -1;
+        s_len[threadIdx.x] = len;
+        __syncthreads();
+        int rank = 0;
+        for (int i = 0; i < n; i += 4) {
+            const int4 x = *reinterpret_cast<const int4*>(&s_len[i]);
+            rank += (x.x > len || (x.x == len && i < (int)threadIdx.x)) + (x.y > len || (x.y == len && i + 1 < (int)threadIdx.x)) +
+                    (x.z > len || (x.z == len && i + 2 < (int)threadIdx.x)) + (x.w > len || (x.w == len && i + 3 < (int)threadIdx.x));
+        }
+        if ((int)threadIdx.x < n && rank == place - base) s_mine = base + threadIdx.x;
+        __syncthreads();
+        unit = __builtin_amdgcn_readfirstlane(s_mine) * c.kv_heads + unit % c.kv_heads;
+    }
+    const int group = c.group, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 15, g = lane >> 4;
+    Tile t;
+    const bool some = unit_of<STEP>(a, unit, tile * ROWS, t);
+    const int r0 = tile * ROWS, r1 = min(t.rows, r0 + ROWS);
 
-    // a step appends its row; nothing reads it from the page in this launch
-    const bool append = a.starts == nullptr && a.k_new != nullptr;
-    const int pos_new = append ? p_lo : -1;
+    // A step's new rows are taken from where they are, by way of LDS: nothing reads them from their page in this launch.
+    const bool append = STEP && a.k_new != nullptr;
     const char* new_k = a.k_new + t.b * a.k_bytes + t.h * a.k_head;
     const char* new_v = a.v_new + t.b * a.v_bytes + t.h * a.v_head;
-    if (append && part == 0 && tile == 0 && wave == WAVES - 1 && pos_new >= 0) {
-        const int page = c.table[t.b * c.table_stride + (pos_new >> c.page_shift)];
-        if ((unsigned)page < (unsigned)c.n_pages && lane < D * TT::BYTES / 16) {
-            const int64_t at = page * c.page_bytes + (pos_new & ((1 << c.page_shift) - 1)) * c.slot_bytes + t.h * c.head_bytes + lane * 16;
-            *reinterpret_cast<u32x4_t*>(c.k + at) = reinterpret_cast<const u32x4_t*>(new_k)[lane];
-            *reinterpret_cast<u32x4_t*>(c.v + at) = reinterpret_cast<const u32x4_t*>(new_v)[lane];
-        }
-    }
+    if (append && lane < 2 * PIECES)
+        s_new[wave][lane] = reinterpret_cast<const u32x4_t*>(lane < PIECES ? new_k : new_v)[lane < PIECES ? lane : lane - PIECES];
 
-    // the lane's row: its position, its query as the second operand of K Q^T
-    const int row = r0 + col;
-    const bool row_ok = row < r1;
-    const int token = min(row, r1 - 1) / group;
-    const int p_row = row_ok ? t.pos0 + token : -1;
+    // the lane's row: its query as the second operand of K Q^T
+    const int row = r0 + col, row_q = min(row, max(r1, 1) - 1);
+    const int token = STEP ? 0 : row_q / group;
     u32x4_t q[KL];
-    {
-        const int head = t.h * group + min(row, r1 - 1) - token * group;
-        const char* src = a.q + (t.q.row0 + token) * a.q_bytes + head * a.q_head + g * 16;
+    if (some) {
+        const char* src = a.q + (t.q.row0 + token) * a.q_bytes + (t.h * group + row_q - token * group) * a.q_head + g * 16;
 #pragma unroll
         for (int kk = 0; kk < KL; ++kk) q[kk] = *reinterpret_cast<const u32x4_t*>(src + kk * 64);
     }
-    const char* kbase = c.k + t.h * c.head_bytes + g * 16;
-    const char* vbase = c.v + t.h * c.head_bytes + col * (VE * TT::BYTES);
-    const int in_page = (1 << c.page_shift) - 1;
 
-    auto slot_of = [&](int blk) { const int i = blk * BK; return i < sp.first ? i : i - sp.first + sp.lo; };
+    const int in_page = (1 << c.page_shift) - 1;
     // page of the tile of 16 slots from `pos` on, as the table says, and -1 for what is none
     const int32_t* table = c.table + t.b * c.table_stride;
     auto entry = [&](int pos) { return load_uniform(table + min(pos >> c.page_shift, c.max_pages - 1)); };
     auto page_of = [&](int pos, int page) { return (unsigned)page < (unsigned)c.n_pages && pos < c.max_slots ? page : -1; };
 
-    float m, l;
-    f32x4_t o[NH][VE];
-    bool careful = false;
-
-    Frag<TT, D> f[2];
+    const char* kh = c.k + t.h * c.head_bytes;
+    const char* vh = c.v + t.h * c.head_bytes;
+    const uint32_t k_off = (uint32_t)(col * (int)c.slot_bytes) + g * 16;
+    uint32_t v_off[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v_off[j] = (uint32_t)((g * 4 + j) * (int)c.slot_bytes) + col * (VE * TT::BYTES);
     // Pages that are not there are loaded as page 0 (it is in the pool) and masked.
-    auto load = [&](Frag<TT, D>& x, int pos, const int (&pages)[NT]) {
-        const char* kr[NT];
-        const char* vr[VK];
-#pragma unroll
-        for (int i = 0; i < NT; ++i) {
-            const int64_t at = max(pages[i], 0) * c.page_bytes;
-            const int pk = pos + i * 16 + col;
-            kr[i] = kbase + at + (pk & in_page) * c.slot_bytes;
-            if (pk == pos_new) kr[i] = new_k + g * 16;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int pv = pos + i * 16 + g * 4 + j;
-                vr[i * 4 + j] = vbase + at + (pv & in_page) * c.slot_bytes;
-                if (pv == pos_new) vr[i * 4 + j] = new_v + col * (VE * TT::BYTES);
-            }
-        }
+    Frag<TT, D> x;
+    auto row0 = [&](int pos, int page) { return max(page, 0) * c.page_bytes + (pos & in_page) * c.slot_bytes; };
+    auto load_k = [&](int pos, const int (&pages)[NT]) {
 #pragma unroll
         for (int i = 0; i < NT; ++i)
 #pragma unroll
-            for (int kk = 0; kk < KL; ++kk) x.k[i][kk] = *reinterpret_cast<const u32x4_t*>(kr[i] + kk * 64);
+            for (int kk = 0; kk < KL; ++kk)
+                x.k[i][kk] = *reinterpret_cast<const u32x4_t*>(kh + row0(pos + i * 16, pages[i]) + k_off + kk * 64);
+    };
+    // (A step reads every row once, and its V rows whole by every load: non-temporal.  K rows, a half line by every load, are better off without:
+    // 4 x 32768 slots 96 -> 100 us, 64 ragged sequences 154 -> 177.)
+    auto load_v = [&](int pos, const int (&pages)[NT]) {
 #pragma unroll
         for (int j = 0; j < VK; ++j)
 #pragma unroll
-            for (int h = 0; h < NH; ++h) load_words<VW>(vr[j] + h * (16 * VE * TT::BYTES), x.v[j][h]);
+            for (int h = 0; h < NH; ++h)
+                load_words<VW, STEP>(vh + row0(pos + j / 4 * 16, pages[j / 4]) + v_off[j % 4] + h * (16 * VE * TT::BYTES), x.v[j][h]);
     };
 
-    auto use = [&](Frag<TT, D>& x, int pos, const int (&pages)[NT]) {
+    // The blocks go to the parts' waves in turn: where a wave begins does not depend on the length (but under a window), so its first
+    // block is on its way when the length is not known yet.  From there on a block's K rows are requested when those before them have been
+    // used, and its V rows likewise: each has the other's part of the work to arrive in, and takes the registers of the ones before.
+    // Behind the last block that one is loaded again (a load that is there on every path is what the waits are counted by).
+    int pos[3] = {0, 0, 0}, pages[3][NT];          // of the block in use, the one that travels, the one after it
+    auto known = [&](int p, int (&e)[NT]) {
+#pragma unroll
+        for (int i = 0; i < NT; ++i) e[i] = page_of(p + i * 16, e[i]);
+    };
+    const int mine = part * WAVES + wave, stride = a.splits * WAVES;
+    if constexpr (EARLY) {
+        pos[0] = mine * BK;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) pages[0][i] = entry(pos[0] + i * 16);
+        known(pos[0], pages[0]);
+        load_k(pos[0], pages[0]);
+        load_v(pos[0], pages[0]);
+    }
+
+    if (!some) return;
+    const int p_lo = STEP ? t.pos0 : t.pos0 + r0 / group, p_hi = STEP ? t.pos0 : t.pos0 + (r1 - 1) / group;
+    const int window = !EARLY && c.window > 0 ? c.window : 0x40000000;
+    const Span sp = span(a, p_lo, p_hi);
+    if (part >= sp.parts) return;
+    const bool row_ok = row < r1;
+    const int p_row = STEP ? t.pos0 : row_ok ? t.pos0 + token : -1;          // (a step's lanes without a row have the last one's)
+    const int pos_new = append ? p_lo : -1;
+    if (append && part == 0 && tile == 0 && wave == WAVES - 1 && pos_new >= 0) {
+        const int page = page_of(pos_new, entry(pos_new));
+        if (page >= 0 && lane < 2 * PIECES) {
+            char* to = (lane < PIECES ? c.k : c.v) + page * c.page_bytes + (pos_new & in_page) * c.slot_bytes + t.h * c.head_bytes;
+            *reinterpret_cast<u32x4_t*>(to + (lane < PIECES ? lane : lane - PIECES) * 16) = s_new[wave][lane];
+        }
+    }
+    auto slot_of = [&](int blk) { const int i = blk * BK; return EARLY || i < sp.first ? i : i - sp.first + sp.lo; };
+    const int count = mine < sp.blocks ? (sp.blocks - mine + stride - 1) / stride : 0;
+    auto ahead = [&](int k, int& p, int (&e)[NT]) {
+        p = __builtin_amdgcn_readfirstlane(slot_of(mine + stride * min(k, count - 1)));
+#pragma unroll
+        for (int i = 0; i < NT; ++i) e[i] = entry(p + i * 16);
+    };
+    auto shift = [&] {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            pos[x] = pos[x + 1];
+#pragma unroll
+            for (int i = 0; i < NT; ++i) pages[x][i] = pages[x + 1][i];
+        }
+    };
+
+    float m = -INFINITY, l = 0.f;
+    f32x4_t o[NH][VE];
+#pragma unroll
+    for (int h = 0; h < NH; ++h)
+#pragma unroll
+        for (int e = 0; e < VE; ++e) o[h][e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+
+    // one block, and the loads of the next one
+    auto use = [&](int pos, const int (&pages)[NT], int next, const int (&next_pages)[NT]) {
+        const bool fresh = STEP && (unsigned)(pos_new - pos) < (unsigned)BK;
+        if (fresh) {
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+                if (col == pos_new - pos - i * 16)
+#pragma unroll
+                    for (int kk = 0; kk < KL; ++kk) x.k[i][kk] = s_new[wave][g + kk * 4];
+        }
         f32x4_t s[NT];
 #pragma unroll
         for (int i = 0; i < NT; ++i) s[i] = dot_tile<TT, KL>(x.k[i], q);
+        load_k(next, next_pages);
         bool there = true;
 #pragma unroll
         for (int i = 0; i < NT; ++i) there &= pages[i] >= 0;
@@ -174,19 +238,10 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
                     const int p = pos + i * 16 + g * 4 + j;
                     const bool seen = pages[i] >= 0 && p <= p_row && (p > p_row - window || p < c.n_sink);
                     s[i][j] = seen ? s[i][j] : -INFINITY;
-                    // values that no row sees have no effect, whatever they are
-                    const bool any = pages[i] >= 0 && p <= p_hi && (p > p_lo - window || p < c.n_sink);
-#pragma unroll
-                    for (int h = 0; h < NH; ++h)
-#pragma unroll
-                        for (int w = 0; w < VW; ++w) {
-                            uint32_t& word = x.v[i * 4 + j][h][w];
-                            word = any ? word : 0u;
-                        }
                 }
         }
-        if (a.logits && row_ok) {
-            float* dst = a.logits + ((int64_t)unit * group + row) * a.logit_stride + pos + g * 4;
+        if constexpr (LOGITS) {
+            float* dst = a.logits + ((int64_t)unit * group + row_q) * a.logit_stride + pos + g * 4;
 #pragma unroll
             for (int i = 0; i < NT; ++i) *reinterpret_cast<f32x4_t*>(dst + i * 16) = s[i];
         }
@@ -218,28 +273,34 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
                 p[i][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][j], a.scale, -ref));
                 l += p[i][j];
             }
-        if (careful) {
-            // one key after the other, each row what it sees, weights in fp32
+        if (fresh) {
 #pragma unroll
             for (int i = 0; i < NT; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-#pragma unroll 1
-                    for (int gs = 0; gs < 4; ++gs) {
-                        const float w = __shfl(p[i][j], gs * 16 + col);
-                        const int pk = pos + i * 16 + gs * 4 + j;
-                        if (pages[i] >= 0 && pk <= p_row && (pk > p_row - window || pk < c.n_sink)) {
-                            const char* src = c.v + t.h * c.head_bytes + pages[i] * c.page_bytes + (pk & in_page) * c.slot_bytes;
+                    if (g * 4 + j == pos_new - pos - i * 16)
 #pragma unroll
-                            for (int h = 0; h < NH; ++h)
+                        for (int h = 0; h < NH; ++h)
 #pragma unroll
-                                for (int r = 0; r < 4; ++r)
+                            for (int w = 0; w < VW; ++w)
+                                x.v[i * 4 + j][h][w] = reinterpret_cast<const uint32_t*>(&s_new[wave][PIECES])[(h * 16 + col) * VW + w];
+        }
+        if (!full) {
+            // values that no row sees have no effect, whatever they are
 #pragma unroll
-                                    for (int e = 0; e < VE; ++e)
-                                        o[h][e][r] += w * load_elem<TT>(src, h * 16 * VE + (g * 4 + r) * VE + e);
+            for (int i = 0; i < NT; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int p = pos + i * 16 + g * 4 + j;
+                    const bool any = pages[i] >= 0 && p <= p_hi && (p > p_lo - window || p < c.n_sink);
+#pragma unroll
+                    for (int h = 0; h < NH; ++h)
+#pragma unroll
+                        for (int w = 0; w < VW; ++w) {
+                            uint32_t& word = x.v[i * 4 + j][h][w];
+                            word = any ? word : 0u;
                         }
-                    }
-            return;
+                }
         }
         if constexpr (S::HALF) {
             // The weights as a sum of two 16-bit numbers: what is left of them is below 2^-16 (bf16) of a weight.  One number
@@ -272,57 +333,29 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) o[h][e] = mfma_f32(__builtin_bit_cast(float, x.v[j][h][e]), p[0][j], o[h][e]);
         }
+        load_v(next, next_pages);
     };
 
-    // The wave's blocks: begin + wave, and every fourth from there.  The next block travels while one is used; behind the
-    // last one the last is loaded again (a load that is there on every path is what the waits are counted by).
-    const int count = begin + wave < end ? (end - begin - wave + WAVES - 1) / WAVES : 0;
-    int pos[3] = {0, 0, 0}, pages[3][NT];          // of the block in use, the one that travels, the one after it
-    auto ahead = [&](int k, int& p, int (&e)[NT]) {
-        p = __builtin_amdgcn_readfirstlane(slot_of(begin + wave + WAVES * min(k, count - 1)));
-#pragma unroll
-        for (int i = 0; i < NT; ++i) e[i] = entry(p + i * 16);
-    };
-    auto known = [&](int p, int (&e)[NT]) {
-#pragma unroll
-        for (int i = 0; i < NT; ++i) e[i] = page_of(p + i * 16, e[i]);
-    };
-    auto shift = [&] {
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            pos[x] = pos[x + 1];
-#pragma unroll
-            for (int i = 0; i < NT; ++i) pages[x][i] = pages[x + 1][i];
-        }
-    };
-    for (;;) {
-        m = -INFINITY;
-        l = 0.f;
-#pragma unroll
-        for (int h = 0; h < NH; ++h)
-#pragma unroll
-            for (int e = 0; e < VE; ++e) o[h][e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        if (count > 0) {
+    if (count > 0) {
+        if constexpr (!EARLY) {
             ahead(0, pos[0], pages[0]);
-            ahead(1, pos[1], pages[1]);
             known(pos[0], pages[0]);
-            load(f[0], pos[0], pages[0]);
-            for (int k = 0; k < count; k += 2) {
-                known(pos[1], pages[1]);
-                load(f[1], pos[1], pages[1]);
-                ahead(k + 2, pos[2], pages[2]);
-                use(f[0], pos[0], pages[0]);
-                if (k + 1 >= count) break;
-                shift();
-                known(pos[1], pages[1]);
-                load(f[0], pos[1], pages[1]);
-                ahead(k + 3, pos[2], pages[2]);
-                use(f[1], pos[0], pages[0]);
-                shift();
-            }
+            load_k(pos[0], pages[0]);
+            load_v(pos[0], pages[0]);
         }
-        // A value that is not finite spoils the matrix product: it meets weights of 0 of rows that do not see it, and parts of weights
-        // that are 0 or negative.  Sums stay finite otherwise, so if one has not the wave goes over its blocks again, key by key.
+        ahead(1, pos[1], pages[1]);
+        for (int k = 0; k < count; ++k) {
+            known(pos[1], pages[1]);
+            ahead(k + 2, pos[2], pages[2]);
+            use(pos[0], pages[0], pos[1], pages[1]);
+            shift();
+        }
+    }
+
+    // A value that is not finite spoils the matrix product: it meets weights of 0 of rows that do not see it, and parts of weights that are 0
+    // or negative.  Sums stay finite otherwise, so if one has not the wave forms its sums anew, key by key: a lane has a row and a
+    // quarter of the elements.
+    {
         float z = 0.f;
 #pragma unroll
         for (int h = 0; h < NH; ++h)
@@ -330,8 +363,36 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
             for (int e = 0; e < VE; ++e)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) z = __builtin_fmaf(o[h][e][r], 0.f, z);
-        if (careful || !__any(z != 0.f)) break;           // (0 x infinity and 0 x NaN are NaN, which is no 0)
-        careful = true;
+        if (__any(z != 0.f)) {                            // (0 x infinity and 0 x NaN are NaN, which is no 0)
+#pragma unroll
+            for (int h = 0; h < NH; ++h)
+#pragma unroll
+                for (int e = 0; e < VE; ++e) o[h][e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            const char* qr = a.q + (t.q.row0 + token) * a.q_bytes + (t.h * group + row_q - token * group) * a.q_head;
+            const float ref = (m == -INFINITY ? 0.f : m) + BIAS<TT>;
+#pragma unroll 1
+            for (int i = 0; i < count * BK; ++i) {
+                const int p = slot_of(mine + stride * (i / BK)) + i % BK;
+                const int page = page_of(p, entry(p));
+                if (page < 0) continue;
+                const int64_t at = page * c.page_bytes + (p & in_page) * c.slot_bytes;
+                const char* kr = p == pos_new ? new_k : kh + at;
+                const char* vr = p == pos_new ? new_v : vh + at;
+                float dot = 0.f;
+#pragma unroll 1
+                for (int e = g * (D / 4); e < (g + 1) * (D / 4); ++e) dot += load_elem<TT>(qr, e) * load_elem<TT>(kr, e);
+                dot = rows_sum(dot);
+                if (p <= p_row && (p > p_row - window || p < c.n_sink)) {
+                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(dot, a.scale, -ref));
+#pragma unroll
+                    for (int h = 0; h < NH; ++h)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+#pragma unroll
+                            for (int e = 0; e < VE; ++e) o[h][e][r] += w * load_elem<TT>(vr, h * 16 * VE + (g * 4 + r) * VE + e);
+                }
+            }
+        }
     }
 
     // ---- the four waves' sums joined
@@ -341,9 +402,10 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
     float top = s_m[0][col];
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) top = fmaxf(top, s_m[w][col]);
-    const float mine = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+    const float share = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
     const bool direct = sp.parts == 1;
     const int orow = threadIdx.x >> 4, piece = threadIdx.x & 15;           // 16 lanes write a row
+    const bool own = r0 + orow < r1;
     float sum = 0.f, otop = s_m[0][orow];
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) otop = fmaxf(otop, s_m[w][orow]);
@@ -351,7 +413,7 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
     for (int w = 0; w < WAVES; ++w) sum += s_m[w][orow] == -INFINITY ? s_l[w][orow] : s_l[w][orow] * __builtin_amdgcn_exp2f(s_m[w][orow] - otop);
     const float inv = sum != 0.f ? 1.f / sum : 0.f;
     const int64_t cell = ((int64_t)unit * a.tiles + tile) * a.splits + part;
-    const int otoken = min(r0 + orow, r1 - 1) / group, ohead = t.h * group + min(r0 + orow, r1 - 1) - otoken * group;
+    const int otoken = STEP ? 0 : min(r0 + orow, r1 - 1) / group, ohead = t.h * group + min(r0 + orow, r1 - 1) - otoken * group;
     char* dst = a.out + (t.q.row0 + otoken) * a.out_bytes + ohead * a.out_head;
 #pragma unroll
     for (int h = 0; h < NH; ++h) {
@@ -359,7 +421,7 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int e = 0; e < VE; ++e) s_o[wave][col][(g * 4 + r) * VE + e] = o[h][e][r] * mine;
+            for (int e = 0; e < VE; ++e) s_o[wave][col][(g * 4 + r) * VE + e] = o[h][e][r] * share;
         __syncthreads();
         float x[VE];
 #pragma unroll
@@ -368,107 +430,187 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
 #pragma unroll
             for (int w = 1; w < WAVES; ++w) x[e] += s_o[w][orow][piece * VE + e];
         }
+        if (!own) continue;
         if (direct) {
-            if (r0 + orow < r1) {
-                uint32_t w[VW];
+            uint32_t w[VW];
 #pragma unroll
-                for (int e = 0; e < VW; ++e) {
-                    if constexpr (S::HALF) w[e] = pack2<TT>(mean<TT>(x[2 * e], inv), mean<TT>(x[2 * e + 1], inv));
-                    else w[e] = __builtin_bit_cast(uint32_t, mean<TT>(x[e], inv));
-                }
-                store_words<VW>(dst + (h * 16 + piece) * (VE * TT::BYTES), w);
+            for (int e = 0; e < VW; ++e) {
+                if constexpr (S::HALF) w[e] = pack2<TT>(mean<TT>(x[2 * e], inv), mean<TT>(x[2 * e + 1], inv));
+                else w[e] = __builtin_bit_cast(uint32_t, mean<TT>(x[e], inv));
             }
+            store_words<VW>(dst + (h * 16 + piece) * (VE * TT::BYTES), w);
         } else {
             float* p = a.part + (cell * ROWS + orow) * D + (h * 16 + piece) * VE;
 #pragma unroll
             for (int e = 0; e < VE; e += 4) *reinterpret_cast<f32x4_t*>(p + e) = f32x4_t{x[e], x[e + 1], x[e + 2], x[e + 3]};
         }
     }
-    if (piece == 0) {
+    if (piece == 0 && own) {
         if (a.ml) { a.ml[cell * 32 + orow] = otop; a.ml[cell * 32 + 16 + orow] = sum; }
-        if (a.lse && direct && r0 + orow < r1)
+        if (!STEP && a.lse && direct)
             a.lse[(int64_t)(t.q.row0 + otoken) * (c.kv_heads * group) + ohead] = otop == -INFINITY ? INFINITY : otop + BIAS<TT> + __builtin_amdgcn_logf(sum);
     }
 }
 
 // ---------------------------------------------------------------- joining
-constexpr int TALLY = 1024;          // slots whose weights one workgroup sums
+constexpr int TALLY = 512;           // slots whose weights one workgroup sums
 
-// Workgroup x: tile x / per_tile.  The first of a tile joins its parts; with logits, every one sums the weights of TALLY of the
-// keys that the step saw, in the order of span().
-template <class TT, int D>
+// What a row's parts come to: their largest reference and the sum of the weights by it, in all lanes; the lane's part's share.  (Of at
+// most 64 parts, one to a lane.)
+__device__ __forceinline__ void parts_of(const float* ml, int parts, int most, int lane, float& top, float& sum, float& share)
+{
+    // (cells of parts that there are not are in the workspace too: loading them waits for nothing)
+    float m = -INFINITY, l = 0.f;
+    if (lane < most) { m = ml[lane * 32]; l = ml[lane * 32 + 16]; }
+    if (lane >= parts) { m = -INFINITY; l = 0.f; }
+    top = m;
+    top = fmaxf(top, dpp<0xB1>(top)); top = fmaxf(top, dpp<0x4E>(top)); top = fmaxf(top, dpp<0x141>(top)); top = fmaxf(top, dpp<0x140>(top));
+    float x0, x1;
+    lane_pair<16>(top, x0, x1); top = fmaxf(x0, x1);
+    lane_pair<32>(top, x0, x1); top = fmaxf(x0, x1);
+    share = m == -INFINITY ? (l == l ? 0.f : l) : __builtin_amdgcn_exp2f(m - top);
+    sum = rows_sum(row_allsum(m == -INFINITY ? l : l * share));
+}
+
+// The joined row's output, and its log-sum-exp for a prefill whose weights are summed.
+template <class TT, bool STEP>
+__device__ __forceinline__ void put_row(const WkvPagedCall& a, const Tile& t, int row, int x4, f32x4_t y, float top, float sum)
+{
+    const float inv = sum != 0.f ? 1.f / sum : 0.f;
+    const int token = STEP ? 0 : row / a.c.group, head = t.h * a.c.group + row - token * a.c.group;
+    char* dst = a.out + (t.q.row0 + token) * a.out_bytes + head * a.out_head + x4 * (4 * TT::BYTES);
+    if constexpr (TT::BYTES == 2)
+        *reinterpret_cast<uint2*>(dst) = make_uint2(pack2<TT>(mean<TT>(y[0], inv), mean<TT>(y[1], inv)), pack2<TT>(mean<TT>(y[2], inv), mean<TT>(y[3], inv)));
+    else
+        *reinterpret_cast<f32x4_t*>(dst) = f32x4_t{mean<TT>(y[0], inv), mean<TT>(y[1], inv), mean<TT>(y[2], inv), mean<TT>(y[3], inv)};
+    if (!STEP && a.lse && x4 == 0)
+        a.lse[(int64_t)(t.q.row0 + token) * (a.c.kv_heads * a.c.group) + head] = top == -INFINITY ? INFINITY : top + BIAS<TT> + __builtin_amdgcn_logf(sum);
+}
+
+template <bool STEP> __device__ __forceinline__ Span span_of_row(const WkvPagedCall& a, const Tile& t, int row)
+{
+    if constexpr (STEP) return span(a, t.pos0, t.pos0);
+    const int t0 = row & -a.tile_rows, t1 = min(t.rows, t0 + a.tile_rows);          // (the keys were cut into parts for that tile)
+    return span(a, t.pos0 + t0 / a.c.group, t.pos0 + (t1 - 1) / a.c.group);
+}
+
+// Row x of all cells (per_tile of each): a workgroup joins SETS rows of a few parts, D / 4 lanes each.
+constexpr int FEW = 4;
+template <class TT, int D, bool STEP>
 __global__ __launch_bounds__(THREADS)
+void wkv_paged_join_few_kernel(const WkvPagedCall a, int rows, int per_tile)
+{
+    constexpr int LANES = D / 4, SETS = THREADS / LANES;
+    const int x = blockIdx.x * SETS + threadIdx.x / LANES, x4 = threadIdx.x % LANES;
+    if (x >= rows) return;
+    const int at = x % per_tile, cell = x / per_tile, unit = cell / a.tiles, row = (cell - unit * a.tiles) * ROWS + at;
+    Tile t;
+    if (!unit_of<STEP>(a, unit, row, t)) return;
+    const Span sp = span_of_row<STEP>(a, t, row);
+    if (sp.parts == 1) return;
+    const float* ml = a.ml + (int64_t)cell * a.splits * 32 + at;
+    const float* src = a.part + ((int64_t)cell * a.splits * ROWS + at) * D + x4 * 4;
+    float m[FEW], l[FEW], top = -INFINITY, sum = 0.f;
+    f32x4_t v[FEW], y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < FEW; ++i)
+        if (i < sp.parts) {
+            m[i] = ml[i * 32];
+            l[i] = ml[i * 32 + 16];
+            v[i] = *reinterpret_cast<const f32x4_t*>(src + (int64_t)i * ROWS * D);
+        }
+#pragma unroll
+    for (int i = 0; i < FEW; ++i) if (i < sp.parts) top = fmaxf(top, m[i]);
+#pragma unroll
+    for (int i = 0; i < FEW; ++i)
+        if (i < sp.parts) {
+            const float f = m[i] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[i] - top);
+            sum += f * l[i];
+            y += f * v[i];
+        }
+    put_row<TT, STEP>(a, t, row, x4, y, top, sum);
+}
+
+// The same for up to 64 parts, a workgroup a row: its waves' lanes sum parts side by side.
+template <class TT, int D, bool STEP>
+__global__ __launch_bounds__(THREADS, 4)
 void wkv_paged_join_kernel(const WkvPagedCall a, int per_tile)
 {
-    using S = Shape<TT, D>;
-    const int cell = blockIdx.x / per_tile, piece = blockIdx.x - cell * per_tile;
-    const int unit = cell / a.tiles, tile = cell - unit * a.tiles;
+    constexpr int LANES = D / 4, SETS = THREADS / LANES, DEEP = 64 / SETS;         // parts side by side, one after the other
+    __shared__ f32x4_t s_x[SETS][LANES];
+    const int lane = threadIdx.x & 63;
+    const int at = blockIdx.x % per_tile, cell = blockIdx.x / per_tile, unit = cell / a.tiles, row = (cell - unit * a.tiles) * ROWS + at;
+    const float* ml = a.ml + (int64_t)cell * a.splits * 32 + at;
+    const int set = threadIdx.x / LANES, x4 = threadIdx.x % LANES;
+    const float* src = a.part + ((int64_t)cell * a.splits * ROWS + at) * D + x4 * 4;
+    f32x4_t x[DEEP];
+#pragma unroll
+    for (int i = 0; i < DEEP; ++i)
+        if (i * SETS + set < a.splits) x[i] = *reinterpret_cast<const f32x4_t*>(src + (int64_t)(i * SETS + set) * ROWS * D);
     Tile t;
-    if (!unit_of(a, unit, tile * ROWS, t)) return;
-    const int group = a.c.group, r0 = tile * ROWS, r1 = min(t.rows, r0 + ROWS);
-    // the keys were cut into parts for a tile of a.tile_rows rows
-    const int t0 = r0 & -a.tile_rows, t1 = min(t.rows, t0 + a.tile_rows);
-    const int p_lo = t.pos0 + t0 / group, p_hi = t.pos0 + (t1 - 1) / group;
-    const Span sp = span(a, p_lo, p_hi);
-
-    const int row = threadIdx.x >> 4, lane = threadIdx.x & 15;
-    if (piece == 0 && sp.parts > 1 && r0 + row < r1) {
-        const float* ml = a.ml + (int64_t)cell * a.splits * 32 + row;
-        float top = -INFINITY, sum = 0.f;
-        for (int s = 0; s < sp.parts; ++s) top = fmaxf(top, ml[s * 32]);
-        constexpr int N = D / 64;                                          // four elements each
-        f32x4_t x[N] = {};
-        const float* part = a.part + ((int64_t)cell * a.splits * ROWS + row) * D + lane * 4;
-        for (int s = 0; s < sp.parts; ++s) {
-            const float f = ml[s * 32] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml[s * 32] - top);
-            sum += f * ml[s * 32 + 16];
+    if (!unit_of<STEP>(a, unit, row, t)) return;
+    const Span sp = span_of_row<STEP>(a, t, row);
+    if (sp.parts == 1) return;
+    float top, sum, share;
+    parts_of(ml, sp.parts, a.splits, lane, top, sum, share);
+    f32x4_t y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int i = 0; i < N; ++i) x[i] += f * *reinterpret_cast<const f32x4_t*>(part + (int64_t)s * ROWS * D + i * 64);
-        }
-        const float inv = sum != 0.f ? 1.f / sum : 0.f;
-        const int token = (r0 + row) / group, head = t.h * group + r0 + row - token * group;
-        char* dst = a.out + (t.q.row0 + token) * a.out_bytes + head * a.out_head;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            if constexpr (S::HALF)
-                *reinterpret_cast<uint2*>(dst + (i * 16 + lane) * 8) = make_uint2(pack2<TT>(mean<TT>(x[i][0], inv), mean<TT>(x[i][1], inv)),
-                                                                              pack2<TT>(mean<TT>(x[i][2], inv), mean<TT>(x[i][3], inv)));
-            else
-                *reinterpret_cast<f32x4_t*>(dst + (i * 16 + lane) * 16) = f32x4_t{mean<TT>(x[i][0], inv), mean<TT>(x[i][1], inv), mean<TT>(x[i][2], inv), mean<TT>(x[i][3], inv)};
-        }
-        if (a.lse && lane == 0)
-            a.lse[(int64_t)(t.q.row0 + token) * (a.c.kv_heads * group) + head] = top == -INFINITY ? INFINITY : top + BIAS<TT> + __builtin_amdgcn_logf(sum);
+    for (int i = 0; i < DEEP; ++i) {
+        const float f = __shfl(share, i * SETS + set);
+        if (i * SETS + set < sp.parts) y += f * x[i];
     }
-    if (!a.logits) return;
-
-    // a step: every row of the unit is of one token; tile 0's workgroups sum over all of them
-    if (tile != 0) return;
-    const int keys = p_hi < 0 ? 0 : sp.first + p_hi + 1 - sp.lo;
-    const int first = piece * TALLY;
-    if (first >= keys) return;
-    float w[TALLY / THREADS] = {};
-    for (int r = 0; r < group; ++r) {
-        const float* ml = a.ml + ((int64_t)unit * a.tiles + r / ROWS) * a.splits * 32 + r % ROWS;
-        float top = -INFINITY, sum = 0.f;
-        for (int s = 0; s < sp.parts; ++s) top = fmaxf(top, ml[s * 32]);
-        for (int s = 0; s < sp.parts; ++s)
-            sum += ml[s * 32 + 16] * (ml[s * 32] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml[s * 32] - top));
-        const float lse = top == -INFINITY ? INFINITY : top + BIAS<TT> + __builtin_amdgcn_logf(sum);
-        const float* lg = a.logits + ((int64_t)unit * group + r) * a.logit_stride;
+    s_x[set][x4] = y;
+    __syncthreads();
+    if (set > 0) return;
 #pragma unroll
-        for (int i = 0; i < TALLY / THREADS; ++i) {
-            const int j = first + i * THREADS + threadIdx.x;
-            if (j < keys) w[i] += __builtin_amdgcn_exp2f(__builtin_fmaf(lg[j < sp.first ? j : j - sp.first + sp.lo], a.scale, -lse));
+    for (int i = 1; i < SETS; ++i) y += s_x[i][x4];
+    put_row<TT, STEP>(a, t, row, x4, y, top, sum);
+}
+
+// Weights of a step, summed over a unit's heads and added to the slots' sums: a workgroup takes TALLY of the keys that the unit saw,
+// in the order of span().
+constexpr int HEADS = 256;           // heads of a unit whose log-sum-exps are at hand at a time
+template <class TT>
+__global__ __launch_bounds__(THREADS)
+void wkv_paged_tally_kernel(const WkvPagedCall a, int per_unit)
+{
+    __shared__ float s_lse[HEADS];
+    const int unit = blockIdx.x / per_unit, first = blockIdx.x % per_unit * TALLY;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = a.c.group;
+    Tile t;
+    unit_of<true>(a, unit, 0, t);
+    const Span sp = span(a, t.pos0, t.pos0);
+    const int keys = t.pos0 < 0 ? 0 : sp.first + t.pos0 + 1 - sp.lo;
+    if (first >= keys) return;
+    constexpr int N = TALLY / THREADS;
+    float w[N] = {};
+    int at[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int j = min(first + i * THREADS + (int)threadIdx.x, keys - 1);
+        at[i] = j < sp.first ? j : j - sp.first + sp.lo;
+    }
+    for (int g0 = 0; g0 < group; g0 += HEADS) {
+        const int n = min(HEADS, group - g0);
+        for (int r = wave; r < n; r += WAVES) {
+            float top, sum, share;
+            parts_of(a.ml + ((int64_t)unit * a.tiles + (g0 + r) / ROWS) * a.splits * 32 + (g0 + r) % ROWS, sp.parts, a.splits, lane, top, sum, share);
+            if (lane == 0) s_lse[r] = top == -INFINITY ? INFINITY : top + BIAS<TT> + __builtin_amdgcn_logf(sum);
         }
+        __syncthreads();
+        const float* lg = a.logits + ((int64_t)unit * group + g0) * a.logit_stride;
+#pragma unroll 4
+        for (int r = 0; r < n; ++r)
+#pragma unroll
+            for (int i = 0; i < N; ++i) w[i] += __builtin_amdgcn_exp2f(__builtin_fmaf(lg[r * a.logit_stride + at[i]], a.scale, -s_lse[r]));
+        __syncthreads();
     }
     float* sc = a.c.scores + (int64_t)unit * a.c.score_stride;
 #pragma unroll
-    for (int i = 0; i < TALLY / THREADS; ++i) {
-        const int j = first + i * THREADS + threadIdx.x;
-        if (j >= keys) continue;
-        const int p = j < sp.first ? j : j - sp.first + sp.lo;
-        if (p == p_hi && a.k_new) sc[p] = w[i];
-        else sc[p] += w[i];
+    for (int i = 0; i < N; ++i) {
+        if (first + i * THREADS + (int)threadIdx.x >= keys) continue;
+        if (at[i] == t.pos0 && a.k_new) sc[at[i]] = w[i];
+        else sc[at[i]] += w[i];
     }
 }
 
@@ -488,7 +630,7 @@ void wkv_paged_sums_kernel(const WkvPagedCall a, int unit0, int per_unit)
     const WkvPages& c = a.c;
     const int unit = unit0 + blockIdx.x / per_unit;
     Tile t;
-    if (!unit_of(a, unit, 0, t)) return;
+    if (!unit_of<false>(a, unit, 0, t)) return;
     const int window = c.window > 0 ? c.window : 0x40000000, group = c.group;
     const int in_page = (1 << c.page_shift) - 1;
 #pragma unroll 1
@@ -557,7 +699,7 @@ void wkv_paged_append_kernel(const WkvPagedCall a, int row_chunks, int per_seq)
 {
     const WkvPages& c = a.c;
     const int b = blockIdx.x / per_seq;
-    const Seq s = sequence(a, b);
+    const Seq s = sequence<false>(a, b);
     const int64_t i = (int64_t)(blockIdx.x - b * per_seq) * THREADS + threadIdx.x;
     const int per_token = row_chunks * c.kv_heads;
     const int token = (int)(i / per_token), rest = (int)(i - (int64_t)token * per_token);
@@ -585,6 +727,11 @@ template <class F> hipError_t by_type(int dtype, int head_dim, F&& f)
 
 }  // namespace
 
+int64_t wkv_paged_most_keys(const WkvPages& c, int64_t new_tokens)
+{
+    return c.window > 0 ? std::min<int64_t>(c.max_slots, (int64_t)c.window + c.n_sink + new_tokens + 128) : c.max_slots;
+}
+
 void wkv_paged_shape(WkvPagedCall& a, int64_t units, int64_t rows, int64_t most, int dtype, int head_dim)
 {
     a.tiles = (int)((rows + ROWS - 1) / ROWS);
@@ -593,7 +740,16 @@ void wkv_paged_shape(WkvPagedCall& a, int64_t units, int64_t rows, int64_t most,
     a.block = a.many ? (head_dim > 128 ? 32 : 64) : dtype == WKV_FP32 || head_dim > 128 ? 16 : 32;
     a.least = WAVES;
     const int64_t groups = units * ((rows + a.tile_rows - 1) / a.tile_rows), part = (int64_t)a.block * a.least;
-    a.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(512 + groups - 1) / groups, (most + part - 1) / part, 64}));
+    // A workgroup for each of the 256 compute units, or, where parts stay as long as 1024 keys, three, which run side by side (two with wide
+    // rows).  More and shorter parts cost more at their ends than they gain.  us a step with 256 | 512 | 768 | 1024 workgroups wanted:
+    // 16 sequences of 2047 slots, 2 K/V heads for 32 heads 14.5 | 16.8 | 16.8 | 18.6, the same with rows of 512 bytes 20.8 | 22.9 | 29.5 | 32.5,
+    // 1 x 4096, 32 K/V heads 19.1 | 21.5 | 21.9 | 23.9, 8 x 8192 48.8 | 50.8 | 48.6 | 55.7, 4 x 32768 95.8 | 98.0 | 92.7.  Many rows: two side by side (3 x 333
+    // tokens on 6001: 256 workgroups 268, 512 212, 1024 218).
+    auto over = [&](int64_t n) { return (n + groups - 1) / groups; };
+    const int64_t want = a.many ? over(512) : std::max(over(256), std::min(over(768), most / 1024));
+    a.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want, (most + part - 1) / part, 64}));
+    // More workgroups than run at once: the longest sequences first (64 ragged sequences, 1024 workgroups: 157 -> 148 us).
+    a.order = a.c.batch > 1 && groups * a.splits > 768;
 }
 
 hipError_t wkv_launch_paged_append(const WkvPagedCall& a, int dtype, int head_dim, hipStream_t stream)
@@ -621,16 +777,34 @@ hipError_t wkv_launch_paged_attend(const WkvPagedCall& a, int dtype, int head_di
     return by_type(dtype, head_dim, [&](auto t, auto d) {
         using TT = decltype(t);
         constexpr int D = decltype(d)::value;
-        hipError_t e;
-        if (a.many) {
-            e = wkv_launch_paged_flash(a, dtype, head_dim, stream);
-        } else {
-            hipLaunchKernelGGL((wkv_paged_rows_kernel<TT, D>), dim3((unsigned)(units * a.tiles * a.splits)), dim3(THREADS), 0, stream, a);
+        const WkvPages& c = a.c;
+        const dim3 grid((unsigned)(units * a.tiles * a.splits)), block(THREADS);
+        hipError_t e = hipSuccess;
+        // (a workgroup's start is early where all of them start at once)
+        const bool early = c.window == 0 && !a.order;
+        if (a.many) e = wkv_launch_paged_flash(a, dtype, head_dim, stream);
+        else if (a.starts) hipLaunchKernelGGL((wkv_paged_rows_kernel<TT, D, false, false, false>), grid, block, 0, stream, a);
+        else if (early && !a.logits) hipLaunchKernelGGL((wkv_paged_rows_kernel<TT, D, true, true, false>), grid, block, 0, stream, a);
+        else if (early) hipLaunchKernelGGL((wkv_paged_rows_kernel<TT, D, true, true, true>), grid, block, 0, stream, a);
+        else if (!a.logits) hipLaunchKernelGGL((wkv_paged_rows_kernel<TT, D, true, false, false>), grid, block, 0, stream, a);
+        else hipLaunchKernelGGL((wkv_paged_rows_kernel<TT, D, true, false, true>), grid, block, 0, stream, a);
+        if (e == hipSuccess) e = hipGetLastError();
+        if (e == hipSuccess && a.splits > 1) {
+            const int per_tile = (int)std::min<int64_t>(ROWS, (int64_t)a.max_new * a.c.group);
+            const int rows = (int)(units * a.tiles * per_tile);
+            if (a.splits <= FEW) {
+                const dim3 few((unsigned)((rows + THREADS * 4 / D - 1) / (THREADS * 4 / D)));
+                if (a.starts) hipLaunchKernelGGL((wkv_paged_join_few_kernel<TT, D, false>), few, block, 0, stream, a, rows, per_tile);
+                else hipLaunchKernelGGL((wkv_paged_join_few_kernel<TT, D, true>), few, block, 0, stream, a, rows, per_tile);
+            } else {
+                if (a.starts) hipLaunchKernelGGL((wkv_paged_join_kernel<TT, D, false>), dim3(rows), block, 0, stream, a, per_tile);
+                else hipLaunchKernelGGL((wkv_paged_join_kernel<TT, D, true>), dim3(rows), block, 0, stream, a, per_tile);
+            }
             e = hipGetLastError();
         }
-        if (e == hipSuccess && (a.splits > 1 || a.logits)) {
-            const int per_tile = a.logits ? (int)((a.c.max_slots + 64 + TALLY - 1) / TALLY) : 1;
-            hipLaunchKernelGGL((wkv_paged_join_kernel<TT, D>), dim3((unsigned)(units * a.tiles * per_tile)), dim3(THREADS), 0, stream, a, per_tile);
+        if (e == hipSuccess && a.logits) {
+            const int per_unit = (int)((wkv_paged_most_keys(a.c, 1) + TALLY - 1) / TALLY);
+            hipLaunchKernelGGL((wkv_paged_tally_kernel<TT>), dim3((unsigned)(units * per_unit)), block, 0, stream, a, per_unit);
             e = hipGetLastError();
         }
         return e;

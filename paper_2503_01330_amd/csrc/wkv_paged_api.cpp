@@ -56,6 +56,7 @@ int check(const wkv_paged* c)
     const int64_t unit = 16 / elem_bytes(c->dtype);
     if (c->page_stride < 0 || c->slot_stride < 0 || c->head_stride < 0 || (c->page_stride | c->slot_stride | c->head_stride) % unit != 0)
         return fail(WKV_EINVAL, "strides of the pools must be multiples of 16 bytes and not negative");
+    if (c->slot_stride * elem_bytes(c->dtype) > 1 << 26) return fail(WKV_ESIZE, "slot_stride exceeds 2^26 bytes");
     if (c->table_stride < c->max_pages) return fail(WKV_EINVAL, "table_stride %lld is below max_pages %d", (long long)c->table_stride, c->max_pages);
     return WKV_OK;
 }
@@ -77,12 +78,6 @@ WkvPages pages_of(const wkv_paged& p)
     return c;
 }
 
-// Most keys that some query sees, or a tile of queries of up to new_tokens tokens
-int64_t most_keys(const WkvPages& c, int64_t new_tokens)
-{
-    return c.window > 0 ? std::min<int64_t>(c.max_slots, (int64_t)c.window + c.n_sink + new_tokens + 64) : c.max_slots;
-}
-
 // Workspace of an attention call: each piece at a multiple of 256 bytes.
 struct Layout {
     WkvPagedCall shape = {};
@@ -96,7 +91,8 @@ Layout layout(const wkv_paged& p, bool scores, int n_tokens, int max_new, bool s
     const int64_t units = (int64_t)c.batch * c.kv_heads;
     Layout l;
     const int64_t rows = (int64_t)max_new * c.group;
-    wkv_paged_shape(l.shape, units, rows, most_keys(c, std::min(max_new, 128 / c.group + 2)), p.dtype, p.head_dim);
+    l.shape.c = c;
+    wkv_paged_shape(l.shape, units, rows, wkv_paged_most_keys(c, std::min(max_new, 128 / c.group + 2)), p.dtype, p.head_dim);
     auto take = [&](size_t bytes) { const size_t at = l.total; l.total += (bytes + 255) / 256 * 256; return at; };
     const int splits = l.shape.splits;
     const size_t cells = (size_t)units * l.shape.tiles * splits;
@@ -159,6 +155,8 @@ int attend(const wkv_paged* p, const wkv_paged_rows* r, const int32_t* starts, i
     const int64_t units = (int64_t)p->batch * p->kv_heads;
     if (units * a.tiles * a.splits >= 1 << 24)
         return fail(WKV_ESIZE, "%lld row tiles in %d parts: a launch holds fewer than 2^32 threads", (long long)(units * a.tiles), a.splits);
+    if (a.logits && units * ((a.c.max_slots + 1023) / 1024) >= 1 << 23)
+        return fail(WKV_ESIZE, "%lld units of %d slots: a launch holds fewer than 2^32 threads", (long long)units, a.c.max_slots);
     hipError_t e = hipSuccess;
     if (!step && r->k) e = wkv_launch_paged_append(a, p->dtype, p->head_dim, stream);
     if (e == hipSuccess) e = wkv_launch_paged_attend(a, p->dtype, p->head_dim, stream);

@@ -68,11 +68,11 @@ __device__ __forceinline__ int32_t load_uniform(const int32_t* p)
 
 struct Seq { int len, n, row0; };      // tokens held, new ones among them, row of the first of these
 
-__device__ __forceinline__ Seq sequence(const WkvPagedCall& a, int b)
+template <bool STEP> __device__ __forceinline__ Seq sequence(const WkvPagedCall& a, int b)
 {
     Seq s;
     s.len = min(max(a.c.lens[b], 0), a.c.max_slots);
-    if (a.starts) {
+    if constexpr (!STEP) {
         const int lo = min(max(a.starts[b], 0), a.n_tokens), hi = min(max(a.starts[b + 1], lo), a.n_tokens);
         s.row0 = lo;
         s.n = min(hi - lo, a.max_new);
@@ -85,7 +85,7 @@ __device__ __forceinline__ Seq sequence(const WkvPagedCall& a, int b)
 
 // Keys in the order in which a tile goes over them: the first `first` slots, then those from `lo` on up to the tile's last position,
 // both multiples of a block of keys, so that a block is one of slots.
-struct Span { int first, lo, blocks, parts, per; };
+struct Span { int first, lo, blocks, parts, per; };    // (per: blocks of a part, where a part's are next to each other)
 
 __device__ __forceinline__ Span span(const WkvPagedCall& a, int p_lo, int p_hi)
 {
@@ -96,20 +96,20 @@ __device__ __forceinline__ Span span(const WkvPagedCall& a, int p_lo, int p_hi)
     const int keys = p_hi < 0 ? 0 : s.first + p_hi + 1 - s.lo;
     s.blocks = (keys + low) / a.block;
     // parts of at least a.least blocks; every part has some
-    const int parts = max(1, min(a.splits, (s.blocks + a.least - 1) / a.least));
-    s.per = max(1, (s.blocks + parts - 1) / parts);
-    s.parts = max(1, (s.blocks + s.per - 1) / s.per);
+    s.parts = max(1, min(a.splits, (s.blocks + a.least - 1) / a.least));
+    s.per = max(1, (s.blocks + s.parts - 1) / s.parts);
+    if (a.many) s.parts = max(1, (s.blocks + s.per - 1) / s.per);
     return s;
 }
 
 struct Tile { int b, h, rows, pos0; Seq q; };    // rows of the unit; position of the first new token
 
 // The unit's sequence; whether it has the row.
-__device__ __forceinline__ bool unit_of(const WkvPagedCall& a, int unit, int row, Tile& t)
+template <bool STEP> __device__ __forceinline__ bool unit_of(const WkvPagedCall& a, int unit, int row, Tile& t)
 {
     t.b = unit / a.c.kv_heads;
     t.h = unit - t.b * a.c.kv_heads;
-    t.q = sequence(a, t.b);
+    t.q = sequence<STEP>(a, t.b);
     t.rows = t.q.n * a.c.group;
     t.pos0 = t.q.len - t.q.n;
     return row < t.rows;
