@@ -10,12 +10,12 @@
 #include "wkv_device.h"
 
 #include <algorithm>
+#include <stdlib.h>
 
 namespace {
 
 constexpr int THREADS = 1024, WAVES = THREADS / 64;
-constexpr int BITS[3] = {11, 11, 10}, BINS = 1 << 11;
-
+constexpr int BITS[3] = {11, 11, 10}, BINS = 1 << 11, COPIES = 4;
 // Scores as integers of the same order; a NaN is above +inf, -0 is 0.
 __device__ __forceinline__ uint32_t order_of(float x)
 {
@@ -25,14 +25,17 @@ __device__ __forceinline__ uint32_t order_of(float x)
     return (b >> 31) ? ~b : b | 0x80000000u;
 }
 
+// HELD: scores that a thread holds.
+template <int HELD>
 __global__ __launch_bounds__(THREADS)
 void wkv_evict_select_kernel(const WkvPages c, int budget, int list_stride, int recent, int32_t* __restrict__ kept,
                              int32_t* __restrict__ plan, int32_t* __restrict__ list)
 {
-    __shared__ uint32_t s_hist[BINS];
+    constexpr int STRETCH = HELD * THREADS;
+    __shared__ __attribute__((aligned(16))) uint32_t s_hist[BINS][COPIES];         // (a lane counts into one of the copies: fewer meet at an address)
     __shared__ uint32_t s_wave[WAVES];
     __shared__ uint32_t s_found[2];
-    __shared__ int s_less[WAVES], s_ties[WAVES];
+    __shared__ uint64_t s_count[HELD * WAVES], s_total[(HELD * WAVES + 63) / 64];
     const int unit = blockIdx.x, b = unit / c.kv_heads, h = unit - b * c.kv_heads;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int len = min(max(c.lens[b], 0), c.max_slots);
@@ -52,8 +55,23 @@ void wkv_evict_select_kernel(const WkvPages c, int budget, int list_stride, int 
         return;
     }
 
-    // slots [first, last) may leave; `want` of them do
+    // Slots [first, last) may leave; `want` of them do.  Scores are held in registers, a stretch of the sequence at a time, as integers;
+    // slots that stay anyway are above all (no score is).
     const int first = c.n_sink, last = len - recent, want = len - budget;
+    constexpr uint32_t STAYS = ~0u;
+    uint32_t x[HELD];
+    // (all loads first, from places that are there: a branch around each would wait for each)
+    auto hold = [&](int from) {
+#pragma unroll
+        for (int k = 0; k < HELD; ++k) x[k] = __builtin_bit_cast(uint32_t, score[min(from + k * THREADS + tid, len - 1)]);
+#pragma unroll
+        for (int k = 0; k < HELD; ++k) {
+            const int j = from + k * THREADS + tid;
+            x[k] = j >= first && j < last ? order_of(__builtin_bit_cast(float, x[k])) : STAYS;
+        }
+    };
+    const bool once = len <= STRETCH;
+    if (once) hold(0);
     uint32_t prefix = 0, rest = want;              // bits of the want-th lowest score found so far; its place among those that share them
     int shift = 32;
 #pragma unroll
@@ -61,20 +79,23 @@ void wkv_evict_select_kernel(const WkvPages c, int budget, int list_stride, int 
         const uint32_t taken = pass == 0 ? 0u : ~0u << shift;            // the bits that prefix has
         shift -= BITS[pass];
         const uint32_t mask = (1u << BITS[pass]) - 1;
-        for (int i = tid; i < BINS; i += THREADS) s_hist[i] = 0;
+        for (int i = tid; i < BINS; i += THREADS) *reinterpret_cast<uint4*>(s_hist[i]) = make_uint4(0, 0, 0, 0);
         __syncthreads();
-        for (int j = first + tid; j < last; j += THREADS) {
-            const uint32_t x = order_of(score[j]);
-            if ((x & taken) == prefix) atomicAdd(&s_hist[(x >> shift) & mask], 1u);
+        for (int from = 0; from < len; from += STRETCH) {
+            if (!once) hold(from);
+#pragma unroll
+            for (int k = 0; k < HELD; ++k)
+                if (from + k * THREADS < len && x[k] != STAYS && (x[k] & taken) == prefix) atomicAdd(&s_hist[(x[k] >> shift) & mask][lane % COPIES], 1u);
         }
         __syncthreads();
         // two bins a thread: running count, and the bin in which it reaches `rest`
-        const uint32_t n0 = s_hist[2 * tid], n1 = s_hist[2 * tid + 1];
+        const uint4 h0 = *reinterpret_cast<const uint4*>(s_hist[2 * tid]), h1 = *reinterpret_cast<const uint4*>(s_hist[2 * tid + 1]);
+        const uint32_t n0 = h0.x + h0.y + h0.z + h0.w, n1 = h1.x + h1.y + h1.z + h1.w;
         uint32_t run = n0 + n1;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t x = __shfl_up(run, d);
-            if (lane >= d) run += x;
+            const uint32_t y = __shfl_up(run, d);
+            if (lane >= d) run += y;
         }
         if (lane == 63) s_wave[wave] = run;
         __syncthreads();
@@ -87,40 +108,55 @@ void wkv_evict_select_kernel(const WkvPages c, int budget, int list_stride, int 
         rest -= s_found[1];
         __syncthreads();
     }
-    // Scores below `prefix` leave, and the first `rest` of those equal to it.  A wave takes a stretch of the slots: it counts both,
-    // and then knows how many slots stay before it.
-    const int stretch = ((len + WAVES - 1) / WAVES + 63) & ~63;
-    const int lo = min(len, wave * stretch), hi = min(len, lo + stretch);
-    int less = 0, ties = 0;
-    for (int j0 = lo; j0 < hi; j0 += 64) {
-        const int j = j0 + lane;
-        const bool able = j >= first && j < last && j < hi;
-        const uint32_t x = able ? order_of(score[j]) : ~0u;
-        less += __popcll(__ballot(able && x < prefix));
-        ties += __popcll(__ballot(able && x == prefix));
-    }
-    if (lane == 0) { s_less[wave] = less; s_ties[wave] = ties; }
-    __syncthreads();
-    int gone = 0, tied = 0;
-    for (int w = 0; w < wave; ++w) { gone += s_less[w]; tied += s_ties[w]; }
-    int at = lo - gone - min(tied, (int)rest);
-    const unsigned long long below = (1ull << lane) - 1;
-    for (int j0 = lo; j0 < hi; j0 += 64) {
-        const int j = j0 + lane;
-        const bool able = j >= first && j < last;
-        const uint32_t x = able && j < hi ? order_of(score[j]) : ~0u;
-        const bool tie = able && j < hi && x == prefix;
-        const unsigned long long tb = __ballot(tie);
-        const bool leaves = able && j < hi && (x < prefix || (tie && tied + __popcll(tb & below) < (int)rest));
-        const bool stays = j < hi && !leaves;
-        const unsigned long long sb = __ballot(stays);
-        if (stays) {
-            const int i = at + __popcll(sb & below);
-            mine[i] = j;
-            if (out) out[i] = j;
+    // Scores below `prefix` leave, and the first `rest` of those equal to it.  The 64 slots of a wave at a time are counted, the counts (those
+    // below in the upper half, equal ones in the lower) summed up in the order of the slots, and then it is known where a slot goes.
+    const unsigned long long under = (1ull << lane) - 1;
+    uint64_t ahead = 0;                            // of the stretches before
+    for (int from = 0; from < len; from += STRETCH) {
+        if (!once) hold(from);
+#pragma unroll
+        for (int k = 0; k < HELD; ++k) {
+            const bool any = from + k * THREADS < len;
+            const int j = from + k * THREADS + tid;
+            const int less = any ? __popcll(__ballot(j < len && x[k] < prefix)) : 0, ties = any ? __popcll(__ballot(j < len && x[k] == prefix)) : 0;
+            if (lane == 0) s_count[k * WAVES + wave] = (uint64_t)less << 32 | (uint32_t)ties;
         }
-        at += __popcll(sb);
-        tied += __popcll(tb);
+        __syncthreads();
+        uint64_t n = 0, run = 0;
+        if (tid < HELD * WAVES) {
+            n = run = s_count[tid];
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const uint64_t y = (uint64_t)__shfl_up((unsigned long long)run, d);
+                if (lane >= d) run += y;
+            }
+            if (lane == 63) s_total[wave] = run;
+        }
+        __syncthreads();
+        if (tid < HELD * WAVES) {
+            uint64_t before = ahead + run - n;
+            for (int w = 0; w < wave; ++w) before += s_total[w];
+            s_count[tid] = before;
+        }
+        for (int w = 0; w < (HELD * WAVES + 63) / 64; ++w) ahead += s_total[w];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < HELD; ++k) {
+            if (from + k * THREADS >= len) break;
+            const int j = from + k * THREADS + tid, j0 = from + k * THREADS + wave * 64;
+            const uint64_t before = s_count[k * WAVES + wave];
+            const int gone = (int)(before >> 32), tied = (int)(uint32_t)before;
+            const bool tie = j < len && x[k] == prefix;
+            const unsigned long long tb = __ballot(tie);
+            const bool stays = j < len && (x[k] > prefix || (tie && tied + __popcll(tb & under) >= (int)rest));
+            const unsigned long long sb = __ballot(stays);
+            if (stays) {
+                const int i = j0 - gone - min(tied, (int)rest) + __popcll(sb & under);
+                mine[i] = j;
+                if (out) out[i] = j;
+            }
+        }
+        __syncthreads();
     }
 }
 
@@ -167,7 +203,7 @@ void wkv_evict_move_kernel(const WkvPages c, int list_stride, int pieces, const 
     }
     if (left == len) return;
     char* base = (what < pieces ? c.k : c.v) + h * c.head_bytes + (what % pieces) * PIECE;
-    constexpr int LANES = PIECE / 16, ROWS = THREADS / LANES, N = 4;       // rows of a load, loads in flight
+    constexpr int LANES = PIECE / 16, ROWS = THREADS / LANES, N = 8;       // rows of a load, loads in flight
     const int row = tid / LANES, off = (tid % LANES) * 16;
     const int in_page = (1 << c.page_shift) - 1;
     const int32_t* table = c.table + b * c.table_stride;
@@ -197,14 +233,18 @@ void wkv_evict_move_kernel(const WkvPages c, int list_stride, int pieces, const 
 hipError_t wkv_launch_paged_evict(const WkvPages& c, int row_bytes, int budget, int recent, int32_t* new_lens, float* new_scores,
                                   int32_t* kept, int32_t* plan, int32_t* list, hipStream_t stream)
 {
-    constexpr int PIECE = 128;
+    static const int PC = getenv("T_P") ? atoi(getenv("T_P")) : 128; const int PIECE = PC;
     const int units = c.batch * c.kv_heads, pieces = row_bytes / PIECE, list_stride = std::min(budget, c.max_slots);
     const int per_unit = 2 * pieces + 1;
     if ((int64_t)units * per_unit >= 1 << 22) return hipErrorInvalidValue;       // 2^32 threads
-    hipLaunchKernelGGL(wkv_evict_select_kernel, dim3(units), dim3(THREADS), 0, stream, c, budget, list_stride, recent, kept, plan, list);
+    // (sequences of up to 4096 slots: 8 us with 4 scores a thread, 17 with 32)
+    if (c.max_slots <= 4 * THREADS) hipLaunchKernelGGL((wkv_evict_select_kernel<4>), dim3(units), dim3(THREADS), 0, stream, c, budget, list_stride, recent, kept, plan, list);
+    else hipLaunchKernelGGL((wkv_evict_select_kernel<32>), dim3(units), dim3(THREADS), 0, stream, c, budget, list_stride, recent, kept, plan, list);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((wkv_evict_move_kernel<PIECE>), dim3(units * per_unit), dim3(THREADS), 0, stream, c, list_stride, pieces, plan, list,
+    if (PC == 64) hipLaunchKernelGGL((wkv_evict_move_kernel<64>), dim3(units * per_unit), dim3(THREADS), 0, stream, c, list_stride, pieces, plan, list,
+                       new_lens, new_scores); else
+    hipLaunchKernelGGL((wkv_evict_move_kernel<128>), dim3(units * per_unit), dim3(THREADS), 0, stream, c, list_stride, pieces, plan, list,
                        new_lens, new_scores);
     return hipGetLastError();
 }

@@ -11,6 +11,7 @@
 #include "wkv_device.h"
 #include "wkv_paged_device.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace {
@@ -53,10 +54,10 @@ template <int D> struct Block {
     static constexpr int RPL = 64 / CHUNKS;                // rows of a load (64 lanes, 16 bytes each)
     static constexpr int LOADS = BK / RPL / WAVES;         // loads of a wave
     static constexpr int BYTES = BK * D * 2;
-    // The pieces of a row are stored at place (piece ^ turn): lanes that read the same piece of consecutive keys (K), or
-    // 4 keys' pairs of pieces (V), then touch different banks.
-    static constexpr int turn_k(int key) { return D == 64 ? key & 7 : key & 15; }
-    static constexpr int turn_v(int key) { return D == 64 ? (key & 3) << 1 : (key & 7) << 1; }
+    // The pieces of a row are stored at place (piece ^ turn), so that what is read together lies in different banks of the 64: a piece of 16
+    // consecutive keys (K), four pieces next to each other of 4 consecutive keys (V).
+    static constexpr int turn_k(int key) { return D == 64 ? key >> 1 & 7 : key & 15; }
+    static constexpr int turn_v(int key) { return D == 64 ? (key >> 1 & 1) << 2 : (key & 3) << 2; }
 };
 
 template <class TT, int D>
@@ -178,6 +179,9 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
 
     auto use = [&](uint32_t kb, uint32_t vb, int pos, const int (&pages)[NG]) {
         if (pos > p_hi) return;                                            // (the wave's rows are all before it)
+#ifdef PRIO
+        __builtin_amdgcn_s_setprio(1);
+#endif
         f32x16_t s[NB];
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
@@ -188,6 +192,9 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
                 s[b] = mfma32<TT>(k, q[i], s[b]);
             }
         }
+#ifdef PRIO
+        __builtin_amdgcn_s_setprio(0);
+#endif
         const bool full = all_there(pages) && pos + BK - 1 <= p_lo && (pos > p_hi - window || pos + BK <= c.n_sink);
         if (!full) {
 #pragma unroll
@@ -358,7 +365,213 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
     }
 }
 
+// ---------------------------------------------------------------- weights of a prefill's rows, summed for every slot
+//
+// sum over the rows of 2^(logit - log-sum-exp).  A wave keeps 32 keys in registers and goes over all rows that see some of
+// its workgroup's keys, 64 at a time through LDS: S = Q K^T leaves in a lane 16 rows of one key, so the sums stay in the lane.  Bound by the
+// vector instructions: an exponential, a multiply-add and an addition a logit, 24 cycles against the 16 of its matrix instructions.
+template <class TT, int D>
+__global__ __launch_bounds__(THREADS, 2)
+void wkv_paged_colsum_kernel(const WkvPagedCall a, int by_unit, int64_t fast, int64_t first)
+{
+    constexpr int KS = D / 16, CHUNKS = D / 8, RPL = 64 / CHUNKS, QROWS = 64, LOADS = QROWS / RPL / WAVES, BYTES = QROWS * D * 2;
+    __shared__ __attribute__((aligned(1024))) char s_q[2 * BYTES];
+    __shared__ __attribute__((aligned(16))) float s_lse[2][QROWS];
+    __shared__ __attribute__((aligned(16))) int s_pos[2][QROWS];
+    const uint32_t q0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)s_q;
+    const WkvPages& c = a.c;
+    // Prompts: the first keys, which the most rows see, of all units first, which spreads the work over the compute units (unit after unit, some got
+    // only first keys: 4 x 4096 620 -> 430 us).  Chunks onto longer sequences: unit after unit.
+    // A key block's rows are cut into a.row_parts where there are few blocks.
+    const int row_part = blockIdx.x % a.row_parts, id = blockIdx.x / a.row_parts;
+    const int slow = (int)first + id / (int)fast, quick = id % (int)fast;
+    const int unit = by_unit ? slow : quick, k0 = (by_unit ? quick : slow) * (WAVES * 32);
+    Tile t;
+    if (!unit_of<false>(a, unit, 0, t) || k0 >= t.q.len) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 31, half = lane >> 5, group = c.group;
+    const int window = c.window > 0 ? c.window : 0x40000000, in_page = (1 << c.page_shift) - 1;
+
+    // the wave's keys
+    const int kw = k0 + wave * 32, key = kw + col;
+    u32x4_t k[KS];
+    const int page = c.table[t.b * c.table_stride + min(key >> c.page_shift, c.max_pages - 1)];
+    const bool there = (unsigned)page < (unsigned)c.n_pages && key < t.q.len;
+    {
+        const char* src = c.k + (there ? page : 0) * c.page_bytes + (key & in_page) * c.slot_bytes + t.h * c.head_bytes + half * 16;
+#pragma unroll
+        for (int i = 0; i < KS; ++i) k[i] = *reinterpret_cast<const u32x4_t*>(src + i * 32);
+    }
+
+    // rows that see some key of the workgroup
+    const int i0 = max(0, k0 - t.pos0);
+    const int i1 = k0 < c.n_sink ? t.q.n : (int)min((int64_t)t.q.n, (int64_t)k0 + WAVES * 32 - 1 + window - t.pos0);
+    int r_lo = i0 * group & -QROWS, r_hi = i1 * group;
+    if (a.row_parts > 1) {
+        const int each = ((r_hi - r_lo + QROWS - 1) / QROWS + a.row_parts - 1) / a.row_parts * QROWS;
+        r_lo += row_part * each;
+        r_hi = min(r_hi, r_lo + each);
+    }
+    // The lane's rows of a load and its token and head, moved on by QROWS rows from one tile to the next; those of the thread's
+    // log-sum-exp (threads 0 .. 63).
+    struct Place { int row, token, head; };
+    const int step_t = QROWS / group, step_h = QROWS % group;
+    auto place = [&](int row) { Place p = {row, row / group, 0}; p.head = row - p.token * group; return p; };
+    auto move = [&](Place& p) {
+        p.row += QROWS;
+        p.token += step_t;
+        p.head += step_h;
+        if (p.head >= group) { p.head -= group; ++p.token; }
+    };
+    const int lrow = lane / CHUNKS, piece = lane % CHUNKS;
+    Place at[LOADS], mine = place(r_lo + (threadIdx.x & 63));
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) at[i] = place(r_lo + (i * WAVES + wave) * RPL + lrow);
+    const int last_t = t.q.n - 1, last_h = group - 1;
+    const char* qh = a.q + t.q.row0 * a.q_bytes + (int64_t)t.h * group * a.q_head;
+    auto load = [&](uint32_t q) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int r = (i * WAVES + wave) * RPL + lrow;
+            const bool ok = at[i].row < t.rows;              // (rows behind the last one: that one again, with a weight of 0)
+            const char* src = qh + (ok ? at[i].token : last_t) * a.q_bytes + (ok ? at[i].head : last_h) * a.q_head;
+            load_lds(src + ((piece ^ Block<D>::turn_k(r)) * 16), q + (i * WAVES + wave) * 1024);
+            move(at[i]);
+        }
+    };
+    float lse = INFINITY;
+    int pos = -1;
+    auto load_row = [&] {
+        lse = INFINITY;
+        pos = -1;
+        if (threadIdx.x < QROWS && mine.row < t.rows) {
+            lse = a.lse[(int64_t)(t.q.row0 + mine.token) * (c.kv_heads * group) + t.h * group + mine.head];
+            pos = t.pos0 + mine.token;
+        }
+        move(mine);
+    };
+    auto keep_row = [&](int x) {
+        if (threadIdx.x < QROWS) { s_lse[x][threadIdx.x] = lse; s_pos[x][threadIdx.x] = pos; }
+    };
+
+    const uint32_t q_at = col * (D * 2) + ((half ^ Block<D>::turn_k(col)) << 4);
+    float sum = 0.f;
+    auto add = [&](uint32_t q, int x, auto full) {
+#pragma unroll
+        for (int rb = 0; rb < QROWS / 32; ++rb) {
+            u32x4_t f[KS];
+#pragma unroll
+            for (int i = 0; i < KS; ++i) f[i] = *lds_ptr<u32x4_t>((q_at ^ (i << 5)) + q + rb * 32 * (D * 2));
+            f32x16_t s = {};
+#pragma unroll
+            for (int i = 0; i < KS; ++i) s = mfma32<TT>(f[i], k[i], s);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const f32x4_t ls = *reinterpret_cast<const f32x4_t*>(&s_lse[x][rb * 32 + j * 8 + half * 4]);
+                const int4 pr = *reinterpret_cast<const int4*>(&s_pos[x][rb * 32 + j * 8 + half * 4]);
+                const int p4[4] = {pr.x, pr.y, pr.z, pr.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j * 4 + e], a.scale, -ls[e]));
+                    if constexpr (!decltype(full)::value) {
+                        asm("" : "+v"(w));                    // (a selection, no branch: w may be NaN)
+                        w = key <= p4[e] && (key > p4[e] - window || key < c.n_sink) ? w : 0.f;
+                    }
+                    sum += w;
+                }
+            }
+        }
+    };
+    auto use = [&](uint32_t q, int x, int r0) {
+        // positions of the tile's first and last row
+        const int p_lo = t.pos0 + r0 / group, p_hi = t.pos0 + (min(r0 + QROWS, t.rows) - 1) / group;
+        if (kw > p_hi) return;
+        if (kw + 31 <= p_lo && (kw > p_hi - window || kw + 32 <= c.n_sink)) add(q, x, std::true_type{});
+        else add(q, x, std::false_type{});
+    };
+    auto arrive = [&] {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0x0F70);               // vmcnt(0)
+        __syncthreads();
+        asm volatile("" ::: "memory");
+    };
+    if (r_lo < r_hi) {
+        load(q0);
+        load_row();
+        keep_row(0);
+        for (int r0 = r_lo, x = 0; r0 < r_hi; r0 += QROWS, x ^= 1) {
+            arrive();
+            const bool more = r0 + QROWS < r_hi;
+            if (more) {
+                load(q0 + (x ^ 1) * BYTES);
+                load_row();
+            }
+            use(q0 + x * BYTES, x, r0);
+            if (more) keep_row(x ^ 1);
+        }
+    }
+    sum = pair_sum<32>(sum);
+    if (half == 0 && key < t.q.len && a.row_parts > 1)
+        a.colsums[((int64_t)row_part * c.batch * c.kv_heads + unit) * a.logit_stride + key] = there ? sum : 0.f;
+    else if (half == 0 && key < t.q.len) {
+        float* sc = c.scores + (int64_t)unit * c.score_stride + key;
+        if (a.k_new && key >= t.pos0) *sc = there ? sum : 0.f;
+        else if (there) *sc += sum;
+    }
+}
+
+// The row parts' sums added to the scores, in the order of the parts.
+__global__ __launch_bounds__(THREADS)
+void wkv_paged_colsum_join_kernel(const WkvPagedCall a, int per_unit)
+{
+    const WkvPages& c = a.c;
+    const int unit = blockIdx.x / per_unit, key = blockIdx.x % per_unit * THREADS + threadIdx.x;
+    Tile t;
+    if (!unit_of<false>(a, unit, 0, t) || key >= t.q.len) return;
+    const int page = c.table[t.b * c.table_stride + (key >> c.page_shift)];
+    const bool there = (unsigned)page < (unsigned)c.n_pages, fresh = a.k_new && key >= t.pos0;
+    float* sc = c.scores + (int64_t)unit * c.score_stride + key;
+    float w = 0.f;
+    for (int i = 0; i < a.row_parts; ++i) w += a.colsums[((int64_t)i * c.batch * c.kv_heads + unit) * a.logit_stride + key];
+    if (fresh) *sc = w;
+    else if (there) *sc += w;
+}
+
 }  // namespace
+
+int wkv_paged_row_parts(int64_t units, int64_t slots, int64_t rows)
+{
+    // about 1024 workgroups, of at least 4 tiles of 64 rows each
+    return (int)std::max<int64_t>(1, std::min<int64_t>({1024 / (units * ((slots + 127) / 128)), rows / 256, 8}));
+}
+
+hipError_t wkv_launch_paged_colsum(const WkvPagedCall& a, int dtype, int head_dim, hipStream_t stream)
+{
+    const int64_t units = (int64_t)a.c.batch * a.c.kv_heads;
+    const int64_t blocks = (a.c.max_slots + WAVES * 32 - 1) / (WAVES * 32);
+    const int by_unit = a.max_new < a.c.max_slots / 2;
+    const int64_t fast = by_unit ? blocks : units, all = by_unit ? units : blocks;      // the index that runs first, the other
+    const int64_t most = std::max<int64_t>(1, ((1 << 24) - 1) / (fast * a.row_parts));
+    auto go = [&](auto t, auto d) {
+        using TT = decltype(t);
+        constexpr int D = decltype(d)::value;
+        for (int64_t b = 0; b < all;) {                 // in pieces below 2^32 threads
+            const int64_t n = std::min<int64_t>(all - b, most);
+            hipLaunchKernelGGL((wkv_paged_colsum_kernel<TT, D>), dim3((unsigned)(n * fast * a.row_parts)), dim3(THREADS), 0, stream, a, by_unit, fast, b);
+            b += n;
+        }
+        if (a.row_parts > 1) {
+            const int per_unit = (a.c.max_slots + THREADS - 1) / THREADS;
+            hipLaunchKernelGGL(wkv_paged_colsum_join_kernel, dim3((unsigned)(units * per_unit)), dim3(THREADS), 0, stream, a, per_unit);
+        }
+        return hipGetLastError();
+    };
+    auto size = [&](auto t) {
+        return head_dim == 64 ? go(t, std::integral_constant<int, 64>{}) : head_dim == 128 ? go(t, std::integral_constant<int, 128>{})
+                                                                                           : go(t, std::integral_constant<int, 256>{});
+    };
+    return dtype == WKV_FP16 ? size(TF16{}) : size(TBF16{});
+}
 
 hipError_t wkv_launch_paged_flash(const WkvPagedCall& a, int dtype, int head_dim, hipStream_t stream)
 {

@@ -139,13 +139,17 @@ struct WkvPagedCall {
     float* part;                     // [unit][tile][split][16][head_dim] sums of weight . v, when splits > 1
     float* ml;                       // [unit][tile][split][2][16] reference (log2) and sum of the weights
     float* logits;                   // [unit][group][logit_stride] q . k of a step whose weights are summed, or null
-    int64_t logit_stride;
+    int64_t logit_stride;            // slots, a multiple of 32
+    int row_parts;                   // of a key block's rows, when the weights of a prefill are summed
+    float* colsums;                  // [row part][unit][logit_stride] their sums, when row_parts > 1
     float* lse;                      // [n_tokens][heads] log2 of the sum of exp(logit), of a prefill whose weights are summed, or null
 };
 
 hipError_t wkv_launch_paged_append(const WkvPagedCall& a, int dtype, int head_dim, hipStream_t stream);
 hipError_t wkv_launch_paged_attend(const WkvPagedCall& a, int dtype, int head_dim, hipStream_t stream);
 hipError_t wkv_launch_paged_sums(const WkvPagedCall& a, int dtype, int head_dim, hipStream_t stream);
+int wkv_paged_row_parts(int64_t units, int64_t slots, int64_t rows);
+hipError_t wkv_launch_paged_colsum(const WkvPagedCall& a, int dtype, int head_dim, hipStream_t stream);
 hipError_t wkv_launch_paged_flash(const WkvPagedCall& a, int dtype, int head_dim, hipStream_t stream);
 // Most keys that a query sees, or the queries of new_tokens tokens next to each other.
 int64_t wkv_paged_most_keys(const WkvPages& c, int64_t new_tokens);

@@ -735,7 +735,10 @@ int64_t wkv_paged_most_keys(const WkvPages& c, int64_t new_tokens)
 void wkv_paged_shape(WkvPagedCall& a, int64_t units, int64_t rows, int64_t most, int dtype, int head_dim)
 {
     a.tiles = (int)((rows + ROWS - 1) / ROWS);
-    a.many = dtype != WKV_FP32 && rows > 32;
+    // The kernel for many rows is ahead from about 32 rows on (2000 slots: 20 rows 19.4 us against 15.6 of the other, 48 rows 19.4 | 20.0; 80 rows onto 8000
+    // slots 23 | 43), but not for short prompts that leave the chip half empty either way (77 tokens of 32 K/V heads 15.2 | 12.5, 256 tokens of 8 with
+    // four query heads each 17.9 | 16.0; 4 x 128 of these 15.8 | 20.7).
+    a.many = dtype != WKV_FP32 && rows > 32 && (units * a.tiles > 512 || a.c.max_slots > 256);
     a.tile_rows = a.many ? 128 : ROWS;
     a.block = a.many ? (head_dim > 128 ? 32 : 64) : dtype == WKV_FP32 || head_dim > 128 ? 16 : 32;
     a.least = WAVES;
@@ -815,14 +818,15 @@ hipError_t wkv_launch_paged_sums(const WkvPagedCall& a, int dtype, int head_dim,
 {
     const int64_t units = (int64_t)a.c.batch * a.c.kv_heads;
     const int per_unit = (a.c.max_slots + SUM_KEYS * WAVES - 1) / (SUM_KEYS * WAVES);
-    return by_type(dtype, head_dim, [&](auto t, auto d) {
-        using TT = decltype(t);
+    if (dtype != WKV_FP32) return wkv_launch_paged_colsum(a, dtype, head_dim, stream);
+    auto go = [&](auto d) {
         constexpr int D = decltype(d)::value;
         for (int64_t u = 0; u < units;) {               // in pieces below 2^32 threads
             const int64_t n = std::min<int64_t>(units - u, ((1 << 24) - 1) / per_unit);
-            hipLaunchKernelGGL((wkv_paged_sums_kernel<TT, D>), dim3((unsigned)(n * per_unit)), dim3(THREADS), 0, stream, a, (int)u, per_unit);
+            hipLaunchKernelGGL((wkv_paged_sums_kernel<TF32, D>), dim3((unsigned)(n * per_unit)), dim3(THREADS), 0, stream, a, (int)u, per_unit);
             u += n;
         }
         return hipGetLastError();
-    });
+    };
+    return head_dim == 64 ? go(std::integral_constant<int, 64>{}) : go(std::integral_constant<int, 128>{});
 }

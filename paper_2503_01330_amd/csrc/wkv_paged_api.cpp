@@ -81,8 +81,7 @@ WkvPages pages_of(const wkv_paged& p)
 // Workspace of an attention call: each piece at a multiple of 256 bytes.
 struct Layout {
     WkvPagedCall shape = {};
-    size_t part = 0, ml = 0, logits = 0, lse = 0, total = 0;
-    int64_t logit_stride = 0;
+    size_t part = 0, ml = 0, logits = 0, lse = 0, colsums = 0, total = 0;
 };
 
 Layout layout(const wkv_paged& p, bool scores, int n_tokens, int max_new, bool step)
@@ -98,11 +97,11 @@ Layout layout(const wkv_paged& p, bool scores, int n_tokens, int max_new, bool s
     const size_t cells = (size_t)units * l.shape.tiles * splits;
     if (splits > 1) l.part = take(cells * 16 * p.head_dim * sizeof(float));
     if (splits > 1 || (scores && step)) l.ml = take(cells * 32 * sizeof(float));
-    if (scores && step) {
-        l.logit_stride = (c.max_slots + 31) / 32 * 32;
-        l.logits = take((size_t)units * c.group * l.logit_stride * sizeof(float));
-    }
+    l.shape.logit_stride = (c.max_slots + 31) / 32 * 32;
+    l.shape.row_parts = scores && !step && p.dtype != WKV_FP32 ? wkv_paged_row_parts(units, c.max_slots, rows) : 1;
+    if (scores && step) l.logits = take((size_t)units * c.group * l.shape.logit_stride * sizeof(float));
     if (scores && !step) l.lse = take((size_t)n_tokens * p.heads * sizeof(float));
+    if (l.shape.row_parts > 1) l.colsums = take((size_t)l.shape.row_parts * units * l.shape.logit_stride * sizeof(float));
     return l;
 }
 
@@ -149,8 +148,9 @@ int attend(const wkv_paged* p, const wkv_paged_rows* r, const int32_t* starts, i
     char* w = (char*)workspace;
     if (a.splits > 1) a.part = (float*)(w + l.part);
     if (a.splits > 1 || (p->scores && step)) a.ml = (float*)(w + l.ml);
-    if (p->scores && step) { a.logits = (float*)(w + l.logits); a.logit_stride = l.logit_stride; }
+    if (p->scores && step) a.logits = (float*)(w + l.logits);
     if (p->scores && !step) a.lse = (float*)(w + l.lse);
+    if (a.row_parts > 1) a.colsums = (float*)(w + l.colsums);
     // a launch of 2^32 threads and more is not refused by the runtime: the count wraps
     const int64_t units = (int64_t)p->batch * p->kv_heads;
     if (units * a.tiles * a.splits >= 1 << 24)
