@@ -1,7 +1,7 @@
 // Attention of many new tokens over the paged cache (wkv_paged_prefill in include/wkv.h), 16-bit formats.
 //
 // A workgroup of four waves takes 128 rows of a unit (row r: token r / group, head r % group) and goes over the keys that they see, or
-// a part of them, in blocks of 64 (32 with wide heads).  K and V of a block travel from their pages straight into LDS, the next block's
+// a part of them, in blocks of 64 or 32.  K and V of a block travel from their pages straight into LDS, the next block's
 // while one is used.  A wave has 32 rows: S^T = K Q^T on the 32 x 32 x 16 instruction, whose result holds in a lane four consecutive keys
 // of one row at a time, as O^T = V^T P^T takes them for its second operand: weights stay in their lane.  The values' operand, eight keys
 // of one element, is read from LDS transposed.  A softmax with a running reference: the sums are scaled down only where a logit
@@ -48,8 +48,8 @@ __device__ __forceinline__ void load_lds(const char* from, uint32_t lds)
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
 }
 
-template <int D> struct Block {
-    static constexpr int BK = D > 128 ? 32 : 64;           // keys
+template <int D, int KEYS> struct Block {
+    static constexpr int BK = KEYS;
     static constexpr int CHUNKS = D / 8;                   // 16-byte pieces of a row
     static constexpr int RPL = 64 / CHUNKS;                // rows of a load (64 lanes, 16 bytes each)
     static constexpr int LOADS = BK / RPL / WAVES;         // loads of a wave
@@ -60,12 +60,14 @@ template <int D> struct Block {
     static constexpr int turn_v(int key) { return D == 64 ? (key >> 1 & 1) << 2 : (key & 3) << 2; }
 };
 
-template <class TT, int D>
-__global__ __launch_bounds__(THREADS, D > 128 ? 1 : 2)
+// BK: keys of a block, 64 or 32.  With 32 and rows of 256 bytes three workgroups share a compute unit (164 registers, 32 KB), with 64 two (233): the
+// first is ahead where there are that many (4 x 4096 646 -> 622 us, window 1024 over 2 x 8192 373 -> 336), the other where not (2048 tokens 82 | 70).
+template <class TT, int D, int BK>
+__global__ __launch_bounds__(THREADS, D * BK > 4096 ? 2 : 3)
 void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
 {
-    using B = Block<D>;
-    constexpr int BK = B::BK, NB = BK / 32, KS = D / 16, DB = D / 32;
+    using B = Block<D, BK>;
+    constexpr int NB = BK / 32, KS = D / 16, DB = D / 32;
     __shared__ __attribute__((aligned(1024))) char s_kv[4 * B::BYTES];
     const uint32_t s_k0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)s_kv, s_v0 = s_k0 + B::BYTES;
     const uint32_t s_k1 = s_k0 + 2 * B::BYTES, s_v1 = s_k0 + 3 * B::BYTES;
@@ -166,9 +168,9 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
 
     // Where the lane reads: K's piece 2 i + half of key col, V's piece of elements 32 i + (lane & 31) of the key of its four lanes; other
     // keys and pieces are at fixed distances, but for the turn, which flips bits.
-    const uint32_t k_at = col * (D * 2) + ((half ^ B::turn_k(col)) << 4);
+    uint32_t k_at = col * (D * 2) + ((half ^ B::turn_k(col)) << 4);
     const int v_key = half * 4 + ((lane & 15) >> 2);
-    const uint32_t v_at = v_key * (D * 2) + (((((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) ^ B::turn_v(v_key)) << 4) + (lane & 1) * 8;
+    uint32_t v_at = v_key * (D * 2) + (((((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) ^ B::turn_v(v_key)) << 4) + (lane & 1) * 8;
 
     float ref = -INFINITY, l = 0.f;       // log2 of the weights' reference; the sum of the lane's weights
     f32x16_t o[DB];
@@ -179,6 +181,7 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
 
     auto use = [&](uint32_t kb, uint32_t vb, int pos, const int (&pages)[NG]) {
         if (pos > p_hi) return;                                            // (the wave's rows are all before it)
+        asm("" : "+v"(k_at), "+v"(v_at));                 // (addresses made of these are not kept in registers from block to block)
 #ifdef PRIO
         __builtin_amdgcn_s_setprio(1);
 #endif
@@ -435,7 +438,7 @@ void wkv_paged_colsum_kernel(const WkvPagedCall a, int by_unit, int64_t fast, in
             const int r = (i * WAVES + wave) * RPL + lrow;
             const bool ok = at[i].row < t.rows;              // (rows behind the last one: that one again, with a weight of 0)
             const char* src = qh + (ok ? at[i].token : last_t) * a.q_bytes + (ok ? at[i].head : last_h) * a.q_head;
-            load_lds(src + ((piece ^ Block<D>::turn_k(r)) * 16), q + (i * WAVES + wave) * 1024);
+            load_lds(src + ((piece ^ Block<D, 32>::turn_k(r)) * 16), q + (i * WAVES + wave) * 1024);
             move(at[i]);
         }
     };
@@ -454,7 +457,7 @@ void wkv_paged_colsum_kernel(const WkvPagedCall a, int by_unit, int64_t fast, in
         if (threadIdx.x < QROWS) { s_lse[x][threadIdx.x] = lse; s_pos[x][threadIdx.x] = pos; }
     };
 
-    const uint32_t q_at = col * (D * 2) + ((half ^ Block<D>::turn_k(col)) << 4);
+    const uint32_t q_at = col * (D * 2) + ((half ^ Block<D, 32>::turn_k(col)) << 4);
     float sum = 0.f;
     auto add = [&](uint32_t q, int x, auto full) {
 #pragma unroll
@@ -577,15 +580,19 @@ hipError_t wkv_launch_paged_flash(const WkvPagedCall& a, int dtype, int head_dim
 {
     const int units = a.c.batch * a.c.kv_heads, tiles = (a.tiles * ROWS + TILE_ROWS - 1) / TILE_ROWS;
     const int spread = units % 8 == 0;
-    auto go = [&](auto t, auto d) {
+    auto go = [&](auto t, auto d, auto bk) {
         using TT = decltype(t);
-        constexpr int D = decltype(d)::value;
-        hipLaunchKernelGGL((wkv_paged_flash_kernel<TT, D>), dim3((unsigned)((int64_t)units * tiles * a.splits)), dim3(THREADS), 0, stream, a, tiles, spread);
+        constexpr int D = decltype(d)::value, BK = decltype(bk)::value;
+        hipLaunchKernelGGL((wkv_paged_flash_kernel<TT, D, BK>), dim3((unsigned)((int64_t)units * tiles * a.splits)), dim3(THREADS), 0, stream, a, tiles, spread);
         return hipGetLastError();
     };
     auto wide = [&](auto t) {
-        return head_dim == 64 ? go(t, std::integral_constant<int, 64>{}) : head_dim == 128 ? go(t, std::integral_constant<int, 128>{})
-                                                                                           : go(t, std::integral_constant<int, 256>{});
+        constexpr std::integral_constant<int, 32> few{};
+        constexpr std::integral_constant<int, 64> d64{}, many{};
+        constexpr std::integral_constant<int, 128> d128{};
+        if (head_dim == 64) return go(t, d64, many);
+        if (head_dim == 128) return a.block == 64 ? go(t, d128, many) : go(t, d128, few);
+        return go(t, std::integral_constant<int, 256>{}, few);
     };
     return dtype == WKV_FP16 ? wide(TF16{}) : wide(TBF16{});
 }

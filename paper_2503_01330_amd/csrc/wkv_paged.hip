@@ -740,17 +740,25 @@ void wkv_paged_shape(WkvPagedCall& a, int64_t units, int64_t rows, int64_t most,
     // four query heads each 17.9 | 16.0; 4 x 128 of these 15.8 | 20.7).
     a.many = dtype != WKV_FP32 && rows > 32 && (units * a.tiles > 512 || a.c.max_slots > 256);
     a.tile_rows = a.many ? 128 : ROWS;
-    a.block = a.many ? (head_dim > 128 ? 32 : 64) : dtype == WKV_FP32 || head_dim > 128 ? 16 : 32;
+    const int64_t groups = units * ((rows + a.tile_rows - 1) / a.tile_rows);
+    auto over = [&](int64_t n) { return (n + groups - 1) / groups; };
+    auto parts = [&](int64_t want, int64_t least) { return (int)std::max<int64_t>(1, std::min<int64_t>({want, (most + least - 1) / least, 64})); };
+    if (a.many) {
+        // Parts of 384 keys at least, as many as three workgroups a compute unit want; two for a prompt, whose tiles are of different lengths anyway.
+        // us with 256 | 512 | 768 workgroups wanted: 3 x 333 tokens on 6001 190 | 159 | 171, of ragged lengths 185 | 120 | 99, 2 x 500 on 16000 489 | 359 | 336,
+        // 100 on 32000 140 | 106 | 101, 1000 on 8000 255 | 172 | 161, 1300 55 | 51 | 53, 2 x 3000 of 512 bytes 234 | 232 | 271.
+        a.splits = parts(over((int64_t)a.max_new * 2 > a.c.max_slots ? 512 : 768), 384);
+        a.block = head_dim == 64 || (head_dim == 128 && groups * a.splits <= 512) ? 64 : 32;
+        a.least = 384 / a.block;
+        return;
+    }
+    a.block = dtype == WKV_FP32 || head_dim > 128 ? 16 : 32;
     a.least = WAVES;
-    const int64_t groups = units * ((rows + a.tile_rows - 1) / a.tile_rows), part = (int64_t)a.block * a.least;
     // A workgroup for each of the 256 compute units, or, where parts stay as long as 1024 keys, three, which run side by side (two with wide
     // rows).  More and shorter parts cost more at their ends than they gain.  us a step with 256 | 512 | 768 | 1024 workgroups wanted:
     // 16 sequences of 2047 slots, 2 K/V heads for 32 heads 14.5 | 16.8 | 16.8 | 18.6, the same with rows of 512 bytes 20.8 | 22.9 | 29.5 | 32.5,
-    // 1 x 4096, 32 K/V heads 19.1 | 21.5 | 21.9 | 23.9, 8 x 8192 48.8 | 50.8 | 48.6 | 55.7, 4 x 32768 95.8 | 98.0 | 92.7.  Many rows: two side by side (3 x 333
-    // tokens on 6001: 256 workgroups 268, 512 212, 1024 218).
-    auto over = [&](int64_t n) { return (n + groups - 1) / groups; };
-    const int64_t want = a.many ? over(512) : std::max(over(256), std::min(over(768), most / 1024));
-    a.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want, (most + part - 1) / part, 64}));
+    // 1 x 4096, 32 K/V heads 19.1 | 21.5 | 21.9 | 23.9, 8 x 8192 48.8 | 50.8 | 48.6 | 55.7, 4 x 32768 95.8 | 98.0 | 92.7.
+    a.splits = parts(std::max(over(256), std::min(over(768), most / 1024)), (int64_t)a.block * a.least);
     // More workgroups than run at once: the longest sequences first (64 ragged sequences, 1024 workgroups: 157 -> 148 us).
     a.order = a.c.batch > 1 && groups * a.splits > 768;
 }
