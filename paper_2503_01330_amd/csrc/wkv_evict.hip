@@ -10,7 +10,6 @@
 #include "wkv_device.h"
 
 #include <algorithm>
-#include <stdlib.h>
 
 namespace {
 
@@ -56,7 +55,7 @@ void wkv_evict_select_kernel(const WkvPages c, int budget, int list_stride, int 
     }
 
     // Slots [first, last) may leave; `want` of them do.  Scores are held in registers, a stretch of the sequence at a time, as integers;
-    // slots that stay anyway are above all (no score is).
+    // slots that stay anyway, and places behind the last slot, are above all (no score is).
     const int first = c.n_sink, last = len - recent, want = len - budget;
     constexpr uint32_t STAYS = ~0u;
     uint32_t x[HELD];
@@ -85,7 +84,7 @@ void wkv_evict_select_kernel(const WkvPages c, int budget, int list_stride, int 
             if (!once) hold(from);
 #pragma unroll
             for (int k = 0; k < HELD; ++k)
-                if (from + k * THREADS < len && x[k] != STAYS && (x[k] & taken) == prefix) atomicAdd(&s_hist[(x[k] >> shift) & mask][lane % COPIES], 1u);
+                if (from + k * THREADS < len && (pass == 0 || (x[k] & taken) == prefix)) atomicAdd(&s_hist[(x[k] >> shift) & mask][lane % COPIES], 1u);
         }
         __syncthreads();
         // two bins a thread: running count, and the bin in which it reaches `rest`
@@ -116,9 +115,7 @@ void wkv_evict_select_kernel(const WkvPages c, int budget, int list_stride, int 
         if (!once) hold(from);
 #pragma unroll
         for (int k = 0; k < HELD; ++k) {
-            const bool any = from + k * THREADS < len;
-            const int j = from + k * THREADS + tid;
-            const int less = any ? __popcll(__ballot(j < len && x[k] < prefix)) : 0, ties = any ? __popcll(__ballot(j < len && x[k] == prefix)) : 0;
+            const int less = __popcll(__ballot(x[k] < prefix)), ties = __popcll(__ballot(x[k] == prefix));
             if (lane == 0) s_count[k * WAVES + wave] = (uint64_t)less << 32 | (uint32_t)ties;
         }
         __syncthreads();
@@ -140,21 +137,19 @@ void wkv_evict_select_kernel(const WkvPages c, int budget, int list_stride, int 
         }
         for (int w = 0; w < (HELD * WAVES + 63) / 64; ++w) ahead += s_total[w];
         __syncthreads();
+        const uint64_t before = s_count[min(lane, HELD - 1) * WAVES + wave];      // lane k: of the wave's k-th 64 slots
 #pragma unroll
         for (int k = 0; k < HELD; ++k) {
             if (from + k * THREADS >= len) break;
             const int j = from + k * THREADS + tid, j0 = from + k * THREADS + wave * 64;
-            const uint64_t before = s_count[k * WAVES + wave];
-            const int gone = (int)(before >> 32), tied = (int)(uint32_t)before;
-            const bool tie = j < len && x[k] == prefix;
-            const unsigned long long tb = __ballot(tie);
-            const bool stays = j < len && (x[k] > prefix || (tie && tied + __popcll(tb & under) >= (int)rest));
+            const int gone = __builtin_amdgcn_readlane((int)(before >> 32), k), tied = __builtin_amdgcn_readlane((int)(uint32_t)before, k);
+            bool stays = x[k] > prefix;
+            const unsigned long long tb = __ballot(x[k] == prefix);
+            if (tb != 0) stays |= x[k] == prefix && tied + __popcll(tb & under) >= (int)rest;
+            if (from + (k + 1) * THREADS > len) stays &= j < len;
             const unsigned long long sb = __ballot(stays);
-            if (stays) {
-                const int i = j0 - gone - min(tied, (int)rest) + __popcll(sb & under);
-                mine[i] = j;
-                if (out) out[i] = j;
-            }
+            const int i = __builtin_amdgcn_mbcnt_hi((uint32_t)(sb >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)sb, j0 - gone - min(tied, (int)rest)));
+            if (stays) mine[i] = j;
         }
         __syncthreads();
     }
@@ -167,13 +162,15 @@ __device__ __forceinline__ void read_then_write()
     __syncthreads();
 }
 
-// Workgroup x: unit x / (2 * pieces + 1); K's pieces, V's pieces, the sums.
+// Workgroups of a unit: K's pieces, V's pieces, the sums (and the list of what stayed, for the caller).  Units run first, in eights, so
+// that a unit's workgroups are on one of the chip's eight partitions: two pieces share a cache line.
 template <int PIECE>
 __global__ __launch_bounds__(THREADS)
-void wkv_evict_move_kernel(const WkvPages c, int list_stride, int pieces, const int32_t* __restrict__ plan, const int32_t* __restrict__ list,
+void wkv_evict_move_kernel(const WkvPages c, int list_stride, int pieces, int eights, int budget, int32_t* __restrict__ kept, const int32_t* __restrict__ plan, const int32_t* __restrict__ list,
                            int32_t* __restrict__ new_lens, float* new_scores)
 {
-    const int unit = blockIdx.x / (2 * pieces + 1), what = blockIdx.x - unit * (2 * pieces + 1);
+    const int what = blockIdx.x / eights, unit = blockIdx.x - what * eights;
+    if (unit >= c.batch * c.kv_heads) return;
     const int b = unit / c.kv_heads, h = unit - b * c.kv_heads;
     const int tid = threadIdx.x;
     const int len = plan[2 * b], left = plan[2 * b + 1];
@@ -182,6 +179,8 @@ void wkv_evict_move_kernel(const WkvPages c, int list_stride, int pieces, const 
         const float* from = c.scores + (int64_t)unit * c.score_stride;
         float* to = new_scores + (int64_t)unit * c.score_stride;
         if (h == 0 && tid == 0) new_lens[b] = left;
+        if (kept && left != len)
+            for (int i = tid; i < budget; i += THREADS) kept[(int64_t)unit * budget + i] = mine[i];
         constexpr int N = 4;
         for (int i0 = 0; i0 < left; i0 += N * THREADS) {
             float x[N];
@@ -233,18 +232,16 @@ void wkv_evict_move_kernel(const WkvPages c, int list_stride, int pieces, const 
 hipError_t wkv_launch_paged_evict(const WkvPages& c, int row_bytes, int budget, int recent, int32_t* new_lens, float* new_scores,
                                   int32_t* kept, int32_t* plan, int32_t* list, hipStream_t stream)
 {
-    static const int PC = getenv("T_P") ? atoi(getenv("T_P")) : 128; const int PIECE = PC;
+    constexpr int PIECE = 64;         // of 128 bytes, few units leave half the chip idle (4 x 32768 slots of 8 heads to 2048: 18.5 us, 13.5 of 64)
     const int units = c.batch * c.kv_heads, pieces = row_bytes / PIECE, list_stride = std::min(budget, c.max_slots);
-    const int per_unit = 2 * pieces + 1;
-    if ((int64_t)units * per_unit >= 1 << 22) return hipErrorInvalidValue;       // 2^32 threads
+    const int per_unit = 2 * pieces + 1, eights = (units + 7) / 8 * 8;
+    if ((int64_t)eights * per_unit >= 1 << 22) return hipErrorInvalidValue;       // 2^32 threads
     // (sequences of up to 4096 slots: 8 us with 4 scores a thread, 17 with 32)
     if (c.max_slots <= 4 * THREADS) hipLaunchKernelGGL((wkv_evict_select_kernel<4>), dim3(units), dim3(THREADS), 0, stream, c, budget, list_stride, recent, kept, plan, list);
     else hipLaunchKernelGGL((wkv_evict_select_kernel<32>), dim3(units), dim3(THREADS), 0, stream, c, budget, list_stride, recent, kept, plan, list);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (PC == 64) hipLaunchKernelGGL((wkv_evict_move_kernel<64>), dim3(units * per_unit), dim3(THREADS), 0, stream, c, list_stride, pieces, plan, list,
-                       new_lens, new_scores); else
-    hipLaunchKernelGGL((wkv_evict_move_kernel<128>), dim3(units * per_unit), dim3(THREADS), 0, stream, c, list_stride, pieces, plan, list,
-                       new_lens, new_scores);
+    hipLaunchKernelGGL((wkv_evict_move_kernel<PIECE>), dim3(eights * per_unit), dim3(THREADS), 0, stream, c, list_stride, pieces, eights, budget, kept,
+                       plan, list, new_lens, new_scores);
     return hipGetLastError();
 }

@@ -97,19 +97,18 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
     const int begin = part * sp.per, end = min(sp.blocks, begin + sp.per);
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int col = lane & 31, half = lane >> 5;
+    const int col = lane & 31, half_q = lane >> 5;
     const int window = c.window > 0 ? c.window : 0x40000000;
     const int in_page = (1 << c.page_shift) - 1;
 
     // the lane's row, and the positions of the wave's
     const int w0 = r0 + wave * WAVE_ROWS;
-    const int row = w0 + col;
-    const int token = min(row, r1 - 1) / group, head = t.h * group + min(row, r1 - 1) - token * group;
-    const int p_row = row < r1 ? t.pos0 + token : -1;
+    const int row_q = min(w0 + col, r1 - 1), token_q = row_q / group;
+    const int p_row = w0 + col < r1 ? t.pos0 + token_q : -1;
     const int p_lo = t.pos0 + min(w0, r1 - 1) / group, p_hi = t.pos0 + (min(w0 + WAVE_ROWS, r1) - 1) / group;
     u32x4_t q[KS];
     {
-        const char* src = a.q + (t.q.row0 + token) * a.q_bytes + head * a.q_head + half * 16;
+        const char* src = a.q + (t.q.row0 + token_q) * a.q_bytes + (t.h * group + row_q - token_q * group) * a.q_head + half_q * 16;
 #pragma unroll
         for (int s = 0; s < KS; ++s) q[s] = *reinterpret_cast<const u32x4_t*>(src + s * 32);
     }
@@ -168,8 +167,8 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
 
     // Where the lane reads: K's piece 2 i + half of key col, V's piece of elements 32 i + (lane & 31) of the key of its four lanes; other
     // keys and pieces are at fixed distances, but for the turn, which flips bits.
-    uint32_t k_at = col * (D * 2) + ((half ^ B::turn_k(col)) << 4);
-    const int v_key = half * 4 + ((lane & 15) >> 2);
+    uint32_t k_at = col * (D * 2) + ((half_q ^ B::turn_k(col)) << 4);
+    const int v_key = half_q * 4 + ((lane & 15) >> 2);
     uint32_t v_at = v_key * (D * 2) + (((((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) ^ B::turn_v(v_key)) << 4) + (lane & 1) * 8;
 
     float ref = -INFINITY, l = 0.f;       // log2 of the weights' reference; the sum of the lane's weights
@@ -204,7 +203,7 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
             for (int b = 0; b < NB; ++b)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
-                    const int p = pos + b * 32 + (j >> 2) * 8 + half * 4 + (j & 3);
+                    const int p = pos + b * 32 + (j >> 2) * 8 + half_q * 4 + (j & 3);
                     const bool seen = pages[b * 2 + (j >> 3)] >= 0 && p <= p_row && (p > p_row - window || p < c.n_sink);
                     s[b][j] = seen ? s[b][j] : -INFINITY;
                 }
@@ -289,6 +288,11 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
         round(blk, s_k0, s_v0, s_k1, s_v1);
         if (blk + 1 < end) round(blk + 1, s_k1, s_v1, s_k0, s_v0);
     }
+
+    // (the lane's row once more, so that it takes no registers in the loop above)
+    int tid = threadIdx.x;
+    asm("" : "+v"(tid));
+    const int row = w0 + (tid & 31), token = min(row, r1 - 1) / group, head = t.h * group + min(row, r1 - 1) - token * group, half = tid >> 5 & 1;
 
     l = pair_sum<32>(l);
     // A value that is not finite spoils the sums of rows that do not see it (0 x infinity).  They are finite otherwise; if one is not, the wave
