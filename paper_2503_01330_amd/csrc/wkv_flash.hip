@@ -41,10 +41,14 @@ template <class X> __device__ __forceinline__ const __attribute__((address_space
 }
 __device__ __forceinline__ void load_lds(const char* base, uint32_t off, uint32_t lds)
 {
+    const uint64_t b = (uint64_t)base;                    // (the same in all lanes, and so that the compiler knows)
+    base = (const char*)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(b >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)b));
+    lds = __builtin_amdgcn_readfirstlane(lds);
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
 }
 __device__ __forceinline__ void load_lds(const char* from, uint32_t lds)
 {
+    lds = __builtin_amdgcn_readfirstlane(lds);
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
 }
 
@@ -133,33 +137,52 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
         return x;
     };
 
-    const int lrow = lane / B::CHUNKS, lpiece = lane % B::CHUNKS;
     const char* kh = c.k + t.h * c.head_bytes;
     const char* vh = c.v + t.h * c.head_bytes;
-    auto load = [&](uint32_t kb, uint32_t vb, int pos, const int (&pages)[NG]) {
+    // The call's own tokens, from slot `fresh` on, are read from where they are; the tile's workgroup also puts its tokens' rows into their pages,
+    // which nothing here reads.
+    const int fresh = a.k_new ? t.pos0 : 0x7FFFFFFF;
+    const char* kf = a.k_new + t.h * a.k_head + (t.q.row0 - t.pos0) * a.k_bytes;
+    const char* vf = a.v_new + t.h * a.v_head + (t.q.row0 - t.pos0) * a.v_bytes;
+    if (a.k_new && part == 0) append_rows<D * 2, THREADS>(a, t, (r0 + group - 1) / group, min(t.q.n, (r0 + TILE_ROWS + group - 1) / group));
+
+    auto load = [&](uint32_t kb, uint32_t vb, int pos, const int (&pages)[NG]) __attribute__((always_inline)) {
         // every key is one that some row of the tile sees, or at least a finite one
         const bool inside = all_there(pages) && pos + BK - 1 <= t_hi && (pos > t_lo - window || pos + BK <= c.n_sink);
-        const uint32_t down = (uint32_t)(lrow * (int)c.slot_bytes), kl = kb + wave * 1024, vl = vb + wave * 1024;
+        const uint32_t kl = kb + wave * 1024, vl = vb + wave * 1024;
+        int ln = threadIdx.x & 63;                        // (and what follows from it: not kept from block to block)
+        asm volatile("" : "+v"(ln));
+        const int lrow = ln / B::CHUNKS, lpiece = ln % B::CHUNKS;
         // load i: its first row, the lane's, the page (in narrow rows the waves' loads are of two stretches of 16 slots)
         auto first = [&](int i) { return (i * WAVES + wave) * B::RPL; };
         auto page_of = [&](int i) {
             return WAVES * B::RPL > 16 ? (wave * B::RPL >= 16 ? pages[2 * i + 1] : pages[2 * i]) : pages[i * WAVES * B::RPL / 16];
         };
-        if (inside) {
+        if (inside && pos + BK <= fresh) {
+            const uint32_t down = (uint32_t)(lrow * (int)c.slot_bytes);
 #pragma unroll
             for (int i = 0; i < B::LOADS; ++i) {
                 const int64_t at = page_of(i) * c.page_bytes + ((pos + first(i)) & in_page) * c.slot_bytes;
                 load_lds(kh + at, down + ((lpiece ^ B::turn_k(first(i) + lrow)) * 16), kl + i * (WAVES * 1024));
                 load_lds(vh + at, down + ((lpiece ^ B::turn_v(first(i) + lrow)) * 16), vl + i * (WAVES * 1024));
             }
+        } else if (inside && pos >= fresh) {
+            const uint32_t kd = (uint32_t)(lrow * (int)a.k_bytes), vd = (uint32_t)(lrow * (int)a.v_bytes);
+#pragma unroll
+            for (int i = 0; i < B::LOADS; ++i) {
+                load_lds(kf + (pos + first(i)) * a.k_bytes, kd + ((lpiece ^ B::turn_k(first(i) + lrow)) * 16), kl + i * (WAVES * 1024));
+                load_lds(vf + (pos + first(i)) * a.v_bytes, vd + ((lpiece ^ B::turn_v(first(i) + lrow)) * 16), vl + i * (WAVES * 1024));
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < B::LOADS; ++i) {
                 const int page = page_of(i), in = first(i) + lrow, p = pos + in;
-                const int64_t at = max(page, 0) * c.page_bytes + ((pos + first(i)) & in_page) * c.slot_bytes;
-                const bool any = page >= 0 && p <= t_hi && (p > t_lo - window || p < c.n_sink);
-                const char* vs = vh + at + (down + ((lpiece ^ B::turn_v(in)) * 16));
-                load_lds(kh + at + (down + ((lpiece ^ B::turn_k(in)) * 16)), kl + i * (WAVES * 1024));
+                const int64_t at = max(page, 0) * c.page_bytes + (p & in_page) * c.slot_bytes;
+                const bool any = page >= 0 && p <= t_hi && (p > t_lo - window || p < c.n_sink), new_row = p >= fresh && p < t.q.len;
+                const char* ks = new_row ? kf + p * a.k_bytes : kh + at;
+                const char* vs = new_row ? vf + p * a.v_bytes : vh + at;
+                vs += (lpiece ^ B::turn_v(in)) * 16;
+                load_lds(ks + (lpiece ^ B::turn_k(in)) * 16, kl + i * (WAVES * 1024));
                 load_lds(any ? vs : reinterpret_cast<const char*>(zero_row), vl + i * (WAVES * 1024));
             }
         }
@@ -178,7 +201,7 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
 #pragma unroll
         for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
 
-    auto use = [&](uint32_t kb, uint32_t vb, int pos, const int (&pages)[NG]) {
+    auto use = [&](uint32_t kb, uint32_t vb, int pos, const int (&pages)[NG]) __attribute__((always_inline)) {
         if (pos > p_hi) return;                                            // (the wave's rows are all before it)
         asm("" : "+v"(k_at), "+v"(v_at));                 // (addresses made of these are not kept in registers from block to block)
 #ifdef PRIO
@@ -271,7 +294,7 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
         next = slot_of(min(begin + 1, end - 1));
         entries(next, after);
     }
-    auto round = [&](int blk, uint32_t k, uint32_t v, uint32_t k_next, uint32_t v_next) {
+    auto round = [&](int blk, uint32_t k, uint32_t v, uint32_t k_next, uint32_t v_next) __attribute__((always_inline)) {
         arrive();
         known(next, after);
         if (blk + 1 < end) load(k_next, v_next, next, after);
@@ -316,20 +339,22 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
 #pragma unroll 1
             for (int k = 0; k < BK; ++k) {
                 const int p = p0 + k;
-                if (p >= c.max_slots) break;
+                if (p >= t.q.len) break;
                 const int page = load_uniform(table + (p >> c.page_shift));
                 if ((unsigned)page >= (unsigned)c.n_pages) continue;
-                const int64_t at = page * c.page_bytes + (p & in_page) * c.slot_bytes + t.h * c.head_bytes;
+                const int64_t at = page * c.page_bytes + (p & in_page) * c.slot_bytes;
+                const char* kr = p >= fresh ? kf + p * a.k_bytes : kh + at;
+                const char* vr = p >= fresh ? vf + p * a.v_bytes : vh + at;
                 float dot = 0.f;
 #pragma unroll 1
-                for (int e = half * (D / 2); e < (half + 1) * (D / 2); ++e) dot += load_elem<TT>(qr, e) * load_elem<TT>(c.k + at, e);
+                for (int e = half * (D / 2); e < (half + 1) * (D / 2); ++e) dot += load_elem<TT>(qr, e) * load_elem<TT>(kr, e);
                 dot = pair_sum<32>(dot);
                 if (p <= p_row && (p > p_row - window || p < c.n_sink)) {
                     const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(dot, a.scale, minus));
 #pragma unroll
                     for (int i = 0; i < DB; ++i)
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) o[i][j] += w * load_elem<TT>(c.v + at, i * 32 + (j >> 2) * 8 + half * 4 + (j & 3));
+                        for (int j = 0; j < 16; ++j) o[i][j] += w * load_elem<TT>(vr, i * 32 + (j >> 2) * 8 + half * 4 + (j & 3));
                 }
             }
         }

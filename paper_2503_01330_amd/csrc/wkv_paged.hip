@@ -11,7 +11,7 @@
 //   wkv_paged_join   the parts of a row joined (join_few: of few parts).
 //   wkv_paged_tally  the weights of a step summed for every slot, from the logits that wkv_paged_rows left and the parts' sums.
 //   wkv_paged_sums   the weights of a prefill's rows summed for every slot, from the rows' log-sum-exps.
-//   wkv_paged_append new K and V rows into their pages (a step's rows go there inside wkv_paged_rows).
+// New K and V rows go into their pages on the way: a call reads its own tokens from where they are, so nothing waits for that.
 //
 // Softmax statistics, sums of the weights and of weight . v are fp32.
 #include "../../include/wkv.h"
@@ -134,15 +134,22 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
     uint32_t v_off[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) v_off[j] = (uint32_t)((g * 4 + j) * (int)c.slot_bytes) + col * (VE * TT::BYTES);
-    // Pages that are not there are loaded as page 0 (it is in the pool) and masked.
+    // A chunk's own tokens, from slot `fresh` on, are read from where they are.  Pages that are not there are loaded as page 0 (it is in the
+    // pool) and masked.
+    const int fresh = !STEP && a.k_new ? t.pos0 : 0x7FFFFFFF;
+    const char* kf = a.k_new + t.h * a.k_head + (t.q.row0 - t.pos0) * a.k_bytes;
+    const char* vf = a.v_new + t.h * a.v_head + (t.q.row0 - t.pos0) * a.v_bytes;
     Frag<TT, D> x;
     auto row0 = [&](int pos, int page) { return max(page, 0) * c.page_bytes + (pos & in_page) * c.slot_bytes; };
     auto load_k = [&](int pos, const int (&pages)[NT]) {
 #pragma unroll
         for (int i = 0; i < NT; ++i)
 #pragma unroll
-            for (int kk = 0; kk < KL; ++kk)
-                x.k[i][kk] = *reinterpret_cast<const u32x4_t*>(kh + row0(pos + i * 16, pages[i]) + k_off + kk * 64);
+            for (int kk = 0; kk < KL; ++kk) {
+                const char* src = kh + row0(pos + i * 16, pages[i]) + k_off;
+                if (!STEP && pos + i * 16 + col >= fresh && pos + i * 16 + col < t.q.len) src = kf + (pos + i * 16 + col) * a.k_bytes + g * 16;
+                x.k[i][kk] = *reinterpret_cast<const u32x4_t*>(src + kk * 64);
+            }
     };
     // (A step reads every row once, and its V rows whole by every load: non-temporal.  K rows, a half line by every load, are better off without:
     // 4 x 32768 slots 96 -> 100 us, 64 ragged sequences 154 -> 177.)
@@ -150,8 +157,12 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
 #pragma unroll
         for (int j = 0; j < VK; ++j)
 #pragma unroll
-            for (int h = 0; h < NH; ++h)
-                load_words<VW, STEP>(vh + row0(pos + j / 4 * 16, pages[j / 4]) + v_off[j % 4] + h * (16 * VE * TT::BYTES), x.v[j][h]);
+            for (int h = 0; h < NH; ++h) {
+                const int p = pos + j / 4 * 16 + g * 4 + j % 4;
+                const char* src = vh + row0(pos + j / 4 * 16, pages[j / 4]) + v_off[j % 4];
+                if (!STEP && p >= fresh && p < t.q.len) src = vf + p * a.v_bytes + col * (VE * TT::BYTES);
+                load_words<VW, STEP>(src + h * (16 * VE * TT::BYTES), x.v[j][h]);
+            }
     };
 
     // The blocks go to the parts' waves in turn: where a wave begins does not depend on the length (but under a window), so its first
@@ -188,6 +199,8 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
             *reinterpret_cast<u32x4_t*>(to + (lane < PIECES ? lane : lane - PIECES) * 16) = s_new[wave][lane];
         }
     }
+    if (!STEP && a.k_new && part == 0)
+        append_rows<D * TT::BYTES, THREADS>(a, t, (r0 + group - 1) / group, min(t.q.n, (r0 + ROWS + group - 1) / group));
     auto slot_of = [&](int blk) { const int i = blk * BK; return EARLY || i < sp.first ? i : i - sp.first + sp.lo; };
     const int count = mine < sp.blocks ? (sp.blocks - mine + stride - 1) / stride : 0;
     auto ahead = [&](int k, int& p, int (&e)[NT]) {
@@ -376,8 +389,9 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
                 const int page = page_of(p, entry(p));
                 if (page < 0) continue;
                 const int64_t at = page * c.page_bytes + (p & in_page) * c.slot_bytes;
-                const char* kr = p == pos_new ? new_k : kh + at;
-                const char* vr = p == pos_new ? new_v : vh + at;
+                if (p >= t.q.len) continue;
+                const char* kr = p == pos_new ? new_k : p >= fresh ? kf + p * a.k_bytes : kh + at;
+                const char* vr = p == pos_new ? new_v : p >= fresh ? vf + p * a.v_bytes : vh + at;
                 float dot = 0.f;
 #pragma unroll 1
                 for (int e = g * (D / 4); e < (g + 1) * (D / 4); ++e) dot += load_elem<TT>(qr, e) * load_elem<TT>(kr, e);
@@ -693,28 +707,6 @@ void wkv_paged_sums_kernel(const WkvPagedCall a, int unit0, int per_unit)
     }
 }
 
-// ---------------------------------------------------------------- appending a chunk
-__global__ __launch_bounds__(THREADS)
-void wkv_paged_append_kernel(const WkvPagedCall a, int row_chunks, int per_seq)
-{
-    const WkvPages& c = a.c;
-    const int b = blockIdx.x / per_seq;
-    const Seq s = sequence<false>(a, b);
-    const int64_t i = (int64_t)(blockIdx.x - b * per_seq) * THREADS + threadIdx.x;
-    const int per_token = row_chunks * c.kv_heads;
-    const int token = (int)(i / per_token), rest = (int)(i - (int64_t)token * per_token);
-    const int pos = s.len - s.n + token;
-    if (token >= s.n || pos < 0) return;
-    const int page = c.table[b * c.table_stride + (pos >> c.page_shift)];
-    if ((unsigned)page >= (unsigned)c.n_pages) return;
-    const int h = rest / row_chunks, x = rest - h * row_chunks;
-    const int64_t to = page * c.page_bytes + (pos & ((1 << c.page_shift) - 1)) * c.slot_bytes + h * c.head_bytes + x * 16;
-    const u32x4_t k = *reinterpret_cast<const u32x4_t*>(a.k_new + (s.row0 + token) * a.k_bytes + h * a.k_head + x * 16);
-    const u32x4_t v = *reinterpret_cast<const u32x4_t*>(a.v_new + (s.row0 + token) * a.v_bytes + h * a.v_head + x * 16);
-    *reinterpret_cast<u32x4_t*>(c.k + to) = k;
-    *reinterpret_cast<u32x4_t*>(c.v + to) = v;
-}
-
 template <class F> hipError_t by_type(int dtype, int head_dim, F&& f)
 {
     if (dtype == WKV_FP32) return head_dim == 64 ? f(TF32{}, std::integral_constant<int, 64>{}) : f(TF32{}, std::integral_constant<int, 128>{});
@@ -761,25 +753,6 @@ void wkv_paged_shape(WkvPagedCall& a, int64_t units, int64_t rows, int64_t most,
     a.splits = parts(std::max(over(256), std::min(over(768), most / 1024)), (int64_t)a.block * a.least);
     // More workgroups than run at once: the longest sequences first (64 ragged sequences, 1024 workgroups: 157 -> 148 us).
     a.order = a.c.batch > 1 && groups * a.splits > 768;
-}
-
-hipError_t wkv_launch_paged_append(const WkvPagedCall& a, int dtype, int head_dim, hipStream_t stream)
-{
-    const int row_chunks = head_dim * (dtype == WKV_FP32 ? 4 : 2) / 16;
-    const int64_t per_seq = ((int64_t)a.max_new * a.c.kv_heads * row_chunks + THREADS - 1) / THREADS;
-    // in pieces of whole sequences, each launch below 2^32 threads: nothing but the sequence's number depends on the piece
-    for (int b0 = 0; b0 < a.c.batch;) {
-        const int n = (int)std::min<int64_t>(a.c.batch - b0, std::max<int64_t>(1, ((1 << 24) - 1) / per_seq));
-        if (per_seq >= 1 << 24) return hipErrorInvalidValue;
-        WkvPagedCall p = a;
-        p.c.batch = n;
-        p.c.lens += b0;
-        p.c.table += b0 * p.c.table_stride;
-        p.starts += b0;
-        hipLaunchKernelGGL(wkv_paged_append_kernel, dim3((unsigned)(n * per_seq)), dim3(THREADS), 0, stream, p, row_chunks, (int)per_seq);
-        b0 += n;
-    }
-    return hipGetLastError();
 }
 
 hipError_t wkv_launch_paged_attend(const WkvPagedCall& a, int dtype, int head_dim, hipStream_t stream)

@@ -133,6 +133,7 @@ int attend(const wkv_paged* p, const wkv_paged_rows* r, const int32_t* starts, i
                                r->v ? r->v_stride : 0, r->v ? r->v_head_stride : 0};
     for (int64_t s : strides)
         if (s < 0 || s % unit != 0) return fail(WKV_EINVAL, "strides of rows must be multiples of 16 bytes and not negative");
+    if (r->k && std::max(r->k_stride, r->v_stride) * eb > 1 << 26) return fail(WKV_ESIZE, "k_stride and v_stride must not exceed 2^26 bytes");
     if ((n_tokens > 1 && r->out_stride < p->head_dim) || (p->heads > 1 && r->out_head_stride < p->head_dim))
         return fail(WKV_EINVAL, "rows of out must not overlap");
     const bool step = starts == nullptr;
@@ -158,9 +159,7 @@ int attend(const wkv_paged* p, const wkv_paged_rows* r, const int32_t* starts, i
         return fail(WKV_ESIZE, "%lld row tiles in %d parts: a launch holds fewer than 2^32 threads", (long long)(units * a.tiles), a.splits);
     if (a.logits && units * ((a.c.max_slots + 1023) / 1024) >= 1 << 23)
         return fail(WKV_ESIZE, "%lld units of %d slots: a launch holds fewer than 2^32 threads", (long long)units, a.c.max_slots);
-    hipError_t e = hipSuccess;
-    if (!step && r->k) e = wkv_launch_paged_append(a, p->dtype, p->head_dim, stream);
-    if (e == hipSuccess) e = wkv_launch_paged_attend(a, p->dtype, p->head_dim, stream);
+    hipError_t e = wkv_launch_paged_attend(a, p->dtype, p->head_dim, stream);
     if (e == hipSuccess && !step && p->scores) e = wkv_launch_paged_sums(a, p->dtype, p->head_dim, stream);
     return e == hipSuccess ? WKV_OK : fail(WKV_EHIP, "kernel launch: %s", hipGetErrorString(e));
 }

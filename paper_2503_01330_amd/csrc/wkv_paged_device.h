@@ -115,6 +115,25 @@ template <bool STEP> __device__ __forceinline__ bool unit_of(const WkvPagedCall&
     return row < t.rows;
 }
 
+// Tokens [first, last) of the unit's sequence into their pages, where those are there.
+template <int ROW_BYTES, int THREADS>
+__device__ __forceinline__ void append_rows(const WkvPagedCall& a, const Tile& t, int first, int last)
+{
+    constexpr int PIECES = ROW_BYTES / 16;
+    const WkvPages& c = a.c;
+    for (int i = first * PIECES + (int)threadIdx.x; i < last * PIECES; i += THREADS) {
+        const int token = i / PIECES, x = i % PIECES * 16, pos = t.pos0 + token;
+        if (pos < 0) continue;
+        const int page = c.table[t.b * c.table_stride + (pos >> c.page_shift)];
+        if ((unsigned)page >= (unsigned)c.n_pages) continue;
+        const int64_t to = page * c.page_bytes + (pos & ((1 << c.page_shift) - 1)) * c.slot_bytes + t.h * c.head_bytes + x;
+        const u32x4_t k = *reinterpret_cast<const u32x4_t*>(a.k_new + (t.q.row0 + token) * a.k_bytes + t.h * a.k_head + x);
+        const u32x4_t v = *reinterpret_cast<const u32x4_t*>(a.v_new + (t.q.row0 + token) * a.v_bytes + t.h * a.v_head + x);
+        *reinterpret_cast<u32x4_t*>(c.k + to) = k;
+        *reinterpret_cast<u32x4_t*>(c.v + to) = v;
+    }
+}
+
 }  // namespace
 
 #endif
