@@ -306,7 +306,8 @@ typedef struct wkv_paged {
 } wkv_paged;
 
 /* Rows of a call, by token and head: DEVICE, 16-byte aligned; the row of token t and head h starts at element
- * t*stride + h*head_stride.  Strides are multiples of 16 bytes and not negative (0: the same row for all; not for out). */
+ * t*stride + h*head_stride.  Strides are multiples of 16 bytes and not negative (0: the same row for all; not for out); slot_stride
+ * above and k_stride, v_stride are at most 2^26 bytes. */
 typedef struct wkv_paged_rows {
     const void* q;               /* [tokens][heads][head_dim]                                           */
     const void* k;               /* [tokens][kv_heads][head_dim], or NULL (with v): appended already    */
@@ -315,8 +316,9 @@ typedef struct wkv_paged_rows {
     int64_t q_stride, q_head_stride, k_stride, k_head_stride, v_stride, v_head_stride, out_stride, out_head_stride;
 } wkv_paged_rows;
 
-/* Bytes of DEVICE workspace (16-byte aligned) that wkv_paged_step, wkv_paged_evict and a wkv_paged_prefill of up to
- * n_tokens tokens in all and max_new a sequence (0, 0: none) want for this cache; 0 if the description is invalid.
+/* Bytes of DEVICE workspace (16-byte aligned) that wkv_paged_step, wkv_paged_evict and a wkv_paged_prefill with these
+ * n_tokens and max_new (0, 0: none) want for this cache; 0 if the description is invalid.  Fewer tokens with the same
+ * max_new want no more; another max_new, smaller or larger, may.
  * The contents do not matter before a call, nor after it.  Calls that share a workspace must not overlap in time,
  * recorded ones (HIP graphs) included.  Host-only arithmetic; pointers are not looked at, but for scores being NULL or not. */
 size_t wkv_paged_workspace_bytes(const wkv_paged* c, int n_tokens, int max_new);

@@ -367,7 +367,8 @@ class PagedCache:
     def prefill(self, q, k, v, out, starts, max_new, stream=None):
         """A chunk of new tokens for every sequence, tokens starts[b] .. starts[b + 1] of q, out [n_tokens, heads, head_dim] and
         k, v [n_tokens, kv_heads, head_dim] (or both None); starts: int32 [batch + 1] on the GPU; max_new: the longest chunk.  The workspace
-        grows here if it has to (max_tokens and max_new of the constructor reserve it)."""
+        grows here if it has to: a call recorded into a HIP graph follows one of the same sizes, or a constructor with these max_tokens and
+        max_new."""
         stream = self._stream(stream)
         n = q.shape[0]
         self._fill(n, q, k, v, out)

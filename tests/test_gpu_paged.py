@@ -345,3 +345,138 @@ def test_the_binding_refuses_rows_of_another_kind():
         wkv.PagedCache(x["k"], x["v"], x["table"], x["lens"], 4).evict(8, 1, x["lens"], x["scores"])
     torch.cuda.synchronize()
     assert (o == 7.0).all()
+
+
+# ---------------------------------------------------------------- every way that a call's size leads
+@pytest.mark.parametrize("scores", [False, True])
+@pytest.mark.parametrize("dtype,d", [("fp16", 128), ("fp32", 64)])
+def test_steps_of_many_sequences(dtype, d, scores):
+    """More workgroups than run at once (longest sequences first), and more sequences than are put in order together."""
+    g = torch.Generator().manual_seed(5)
+    lens = torch.randint(0, 70, (100,), generator=g).tolist()
+    run(Paged(51, lens, heads=8, kv_heads=8, d=d, dtype=dtype, scores=scores))
+    lens = torch.randint(0, 40, (300,), generator=g).tolist()
+    run(Paged(52, lens, heads=4, kv_heads=4, d=64, dtype=dtype, scores=scores, window=17, sink=2))
+    run(Paged(53, lens, heads=3, kv_heads=3, d=64, dtype=dtype, scores=scores))
+
+
+def test_many_heads_to_a_kv_head():
+    run(Paged(54, [70, 3], heads=300, kv_heads=1, d=64, scores=True))
+    run(Paged(55, [70, 3], [5, 3], heads=300, kv_heads=1, d=64, scores=True))
+
+
+@pytest.mark.parametrize("dtype,d", [("fp16", 64), ("bf16", 128), ("bf16", 256), ("fp32", 128)])
+def test_short_chunks_onto_long_sequences(dtype, d):
+    """The keys are cut into parts, few and many, for both kernels."""
+    for lens, new, heads in (([1200, 90], [3, 2], 4), ([1200, 90], [30, 2], 8), ([2700], [2], 1), ([2700], [40], 4)):
+        run(Paged(56, lens, new, heads=heads, kv_heads=1, d=d, dtype=dtype, page=64, scores=True))
+        run(Paged(57, lens, new, heads=heads, kv_heads=1, d=d, dtype=dtype, page=32, window=900, sink=5))
+
+
+@pytest.mark.parametrize("dtype,d", [("fp16", 128), ("bf16", 64)])
+def test_chunks_of_many_sequences(dtype, d):
+    """More than 512 tiles of rows."""
+    g = torch.Generator().manual_seed(6)
+    lens = torch.randint(33, 60, (70,), generator=g).tolist()
+    run(Paged(58, lens, [min(n, 35) for n in lens], heads=8, kv_heads=8, d=d, dtype=dtype, max_pages=20, scores=True))
+
+
+def test_evict_more_slots_than_a_workgroup_holds():
+    g = torch.Generator().manual_seed(8)
+    n, page, kvh, d = 40000, 4096, 2, 64
+    k = torch.randn(11, page, kvh, d, generator=g).half()
+    p = Paged(59, [1], heads=2, kv_heads=kvh, d=d, page=page, sink=3, scores=True, spare=0, max_pages=10)
+    p.lens, p.k, p.v = [n], k, k.flip(0).contiguous()
+    p.table = torch.randperm(11, generator=g)[:10].to(torch.int32)[None]
+    p.scores = (torch.rand(1, kvh, 10 * page, generator=g) * 5000).floor()
+    _evict(p, 39000, 100)
+    _evict(p, 500, 100, in_place=True)
+
+
+def test_offsets_beyond_32_bits():
+    """A pool whose pages are 2 GiB apart, rows of calls far apart: step, chunk and eviction."""
+    big = torch.empty(5 << 30, dtype=torch.float16, device="cuda")
+    for new in (None, [45, 20]):
+        p = Paged(60, [70, 20], new, heads=4, kv_heads=2, d=64, spare=0, scores=True)
+        x = p.device()
+        n = p.k.shape[0]
+        assert n <= 8
+        view = {"k": big[: 4 << 30], "v": big[1 << 12:]}
+        for w in ("k", "v"):
+            y = view[w].as_strided((n, p.page, p.kv_heads, p.d), ((1 << 29) + 8, 64 * p.kv_heads, 64, 1))
+            y.copy_(x[w])
+            x[w] = y
+        x["cache"] = wkv.PagedCache(x["k"], x["v"], x["table"], x["lens"], p.heads, scores=x["scores"])
+        run(p, x=x)
+    p = _full(Paged(61, [70, 20], heads=2, kv_heads=2, d=64, spare=0, scores=True))
+    x = p.device()
+    for w in ("k", "v"):
+        y = view[w].as_strided((p.k.shape[0], p.page, 2, 64), ((1 << 29) + 8, 128, 64, 1))
+        y.copy_(x[w])
+        x[w] = y
+    cache = wkv.PagedCache(x["k"], x["v"], x["table"], x["lens"], 2, scores=x["scores"])
+    cache.evict(30, 3, x["lens"], x["scores"])
+    torch.cuda.synchronize()
+    _, lens, scores, k, v = paged.evicted(p, 30, 3)
+    assert x["lens"].tolist() == lens and paged.same(x["scores"].cpu(), scores) and paged.same(x["k"].cpu(), k) and paged.same(x["v"].cpu(), v)
+
+
+def test_shared_pages_and_broadcast_rows():
+    """Two sequences with the same first pages; one row for all tokens, by strides of 0."""
+    p = Paged(62, [100, 100], heads=4, kv_heads=2, d=64, page=16, scores=True)
+    p.table[1, :6] = p.table[0, :6]
+    for b in (0, 1):
+        for j in range(96, 99):
+            at = p.where(b, j)
+            p.k[at], p.v[at] = p.k[p.where(0, j)], p.v[p.where(0, j)]
+    run(p)
+    p = Paged(63, [50, 20], [50, 20], heads=4, kv_heads=2, d=64, scores=True)
+    x = p.device()
+    for n in ("q", "k_new", "v_new"):
+        setattr(p, n, getattr(p, n)[:1].expand(p.rows, -1, -1).contiguous())
+        x[n] = x[n][:1].expand(p.rows, -1, -1)
+    x["cache"].prefill(x["q"], x["k_new"], x["v_new"], x["out"], x["starts"], 50)
+    torch.cuda.synchronize()
+    paged.check(p, x)
+
+
+def test_lengths_and_starts_that_do_not_fit():
+    """Lengths below 0 and beyond the table, chunks longer than max_new or than their sequence, starts that decrease or lie
+    outside: all are cut to what is there."""
+    p = Paged(64, [64, 48, 33], heads=4, kv_heads=2, d=64, max_pages=4, scores=True)
+    p.lens[0] = 64
+    x = p.device()
+    x["lens"].copy_(torch.tensor([1 << 20, 48, -7], dtype=torch.int32))
+    p.lens, p.new = [64, 48, 0], [1, 1, 0]
+    p.k_new[2], p.v_new[2] = 0, 0
+    run(p, x=x)
+    p = Paged(65, [40, 30, 20], [5, 30, 20], heads=4, kv_heads=2, d=64, extra_rows=9, scores=True)
+    x = p.device()
+    before = {n: x[n].clone() for n in ("k", "v", "scores")}
+    x["starts"].copy_(torch.tensor([3, 1, -50, 1 << 30], dtype=torch.int32))
+    # sequence 0: from 3 to max(1, 3), none; 1: from 1 to 1, none; 2: from 0 to the end of 64 rows, cut to 25, five more than its 20 slots
+    x["cache"].prefill(x["q"], x["k_new"], x["v_new"], x["out"], x["starts"], 25)
+    torch.cuda.synchronize()
+    p.starts, p.new = [0, 0, 0], [0, 0, 25]
+    p.starts[2] = 0
+    out, tol, sums, stol = p.reference()
+    out[25:] = 7.0
+    paged.close(x["out"], out, tol, "out")
+    paged.close(x["scores"], sums, stol, "scores")
+    k, v = p.appended()
+    assert paged.same(x["k"].cpu(), k) and paged.same(x["v"].cpu(), v) and not paged.same(x["k"], before["k"])
+
+
+def test_the_same_call_gives_the_same_bits():
+    for new in (None, [300, 90]):
+        got = []
+        for _ in range(2):
+            p = Paged(66, [1500, 90], new, heads=8, kv_heads=2, d=128, dtype="bf16", page=64, scores=True)
+            x = p.device()
+            if new is None:
+                x["cache"].step(x["q"], x["k_new"], x["v_new"], x["out"])
+            else:
+                x["cache"].prefill(x["q"], x["k_new"], x["v_new"], x["out"], x["starts"], 300)
+            torch.cuda.synchronize()
+            got.append((x["out"], x["scores"], x["k"]))
+        assert all(paged.same(a, b) for a, b in zip(*got))

@@ -91,6 +91,12 @@ def test_rows_that_are_refused(kw):
     assert prefill(cache(), rows(**kw)) == wkv.WKV_EINVAL
 
 
+def test_strides_that_32_bits_do_not_hold():
+    assert step(cache(slot_stride=(1 << 25) + 8), rows()) == wkv.WKV_ESIZE
+    assert step(cache(), rows(k_stride=(1 << 25) + 8)) == wkv.WKV_ESIZE and prefill(cache(), rows(v_stride=1 << 30)) == wkv.WKV_ESIZE
+    assert step(cache(page_stride=1 << 40, head_stride=1 << 40), rows(q_stride=1 << 40, k_head_stride=1 << 40, out_stride=1 << 40)) == SOUND
+
+
 def test_rows_that_are_not_used_are_not_looked_at():
     work = wkv._lib.wkv_paged_workspace_bytes(C.byref(cache()), 0, 0)
     assert work > 0
