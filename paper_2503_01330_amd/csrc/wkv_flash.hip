@@ -251,7 +251,7 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) o[i][j] *= f;
         }
-        const float minus = -((ref == -INFINITY ? 0.f : ref) + BIAS<TT>);
+        const float minus = ref == -INFINITY ? 0.f : -ref;
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
 #pragma unroll
@@ -318,8 +318,8 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
     const int row = w0 + (tid & 31), token = min(row, r1 - 1) / group, head = t.h * group + min(row, r1 - 1) - token * group, half = tid >> 5 & 1;
 
     l = pair_sum<32>(l);
-    // A value that is not finite spoils the sums of rows that do not see it (0 x infinity).  They are finite otherwise; if one is not, the wave
-    // forms them anew, key by key: a lane has a row and half of its elements.
+    // A value that is not finite spoils the sums of rows that do not see it (0 x infinity), and sums of the largest values may overflow.  If one is
+    // not finite, the wave forms them anew, key by key: a lane has a row and half of its elements.
     float z = 0.f;
 #pragma unroll
     for (int i = 0; i < DB; ++i)
@@ -332,7 +332,9 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
 #pragma unroll
             for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
         const char* qr = a.q + (t.q.row0 + token) * a.q_bytes + head * a.q_head;
-        const float minus = -((ref == -INFINITY ? 0.f : ref) + BIAS<TT>);
+        ref += CAREFUL<TT>;
+        l *= __builtin_amdgcn_exp2f(-CAREFUL<TT>);
+        const float minus = ref == -INFINITY ? 0.f : -ref;
 #pragma unroll 1
         for (int blk = begin; blk < end; ++blk) {
             const int p0 = slot_of(blk);
@@ -393,7 +395,7 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
             ml[16] = l;
         }
         if (a.lse && direct)
-            a.lse[(int64_t)(t.q.row0 + token) * (c.kv_heads * group) + head] = ref == -INFINITY ? INFINITY : ref + BIAS<TT> + __builtin_amdgcn_logf(l);
+            a.lse[(int64_t)(t.q.row0 + token) * (c.kv_heads * group) + head] = ref == -INFINITY ? INFINITY : ref + __builtin_amdgcn_logf(l);
     }
 }
 

@@ -40,19 +40,23 @@ template <class TT, int D> struct Shape {
     static constexpr int VW = VE * TT::BYTES / 4;          // words of a piece
 };
 
-// The product over 16 dwords of a row (a lane's KL loads): 16-bit rows 8 elements a load and instruction, fp32 rows 4 a load.
+// The product over a row (a lane's KL loads): 16-bit rows 8 elements a load and instruction, fp32 rows 4 a load; in fp32 by four sums, whose
+// roundings are half of one's.
 template <class TT, int KL> __device__ __forceinline__ f32x4_t dot_tile(const u32x4_t (&a)[KL], const u32x4_t (&b)[KL])
 {
     f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+    if constexpr (TT::BYTES == 2) {
 #pragma unroll
-    for (int kk = 0; kk < KL; ++kk) {
-        if constexpr (TT::BYTES == 2) {
-            s = mfma<TT>(a[kk], b[kk], s);
-        } else {
+        for (int kk = 0; kk < KL; ++kk) s = mfma<TT>(a[kk], b[kk], s);
+    } else {
+        f32x4_t t[4] = {};
+#pragma unroll
+        for (int kk = 0; kk < KL; ++kk) {
             const f32x4_t x = __builtin_bit_cast(f32x4_t, a[kk]), y = __builtin_bit_cast(f32x4_t, b[kk]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s = mfma_f32(x[e], y[e], s);
+            for (int e = 0; e < 4; ++e) t[e] = mfma_f32(x[e], y[e], t[e]);
         }
+        s = (t[0] + t[1]) + (t[2] + t[3]);
     }
     return s;
 }
@@ -277,7 +281,7 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
 #pragma unroll
                 for (int e = 0; e < VE; ++e) o[h][e] *= f0;
         }
-        const float ref = (m == -INFINITY ? 0.f : m) + BIAS<TT>;
+        const float ref = m == -INFINITY ? 0.f : m;
         float p[NT][4];
 #pragma unroll
         for (int i = 0; i < NT; ++i)
@@ -366,8 +370,8 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
     }
 
     // A value that is not finite spoils the matrix product: it meets weights of 0 of rows that do not see it, and parts of weights that are 0
-    // or negative.  Sums stay finite otherwise, so if one has not the wave forms its sums anew, key by key: a lane has a row and a
-    // quarter of the elements.
+    // or negative; and sums of the largest values may overflow.  If one is not finite, the wave forms its sums anew, key by key: a lane has a row
+    // and a quarter of the elements.
     {
         float z = 0.f;
 #pragma unroll
@@ -382,7 +386,9 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
 #pragma unroll
                 for (int e = 0; e < VE; ++e) o[h][e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
             const char* qr = a.q + (t.q.row0 + token) * a.q_bytes + (t.h * group + row_q - token * group) * a.q_head;
-            const float ref = (m == -INFINITY ? 0.f : m) + BIAS<TT>;
+            m += CAREFUL<TT>;
+            l *= __builtin_amdgcn_exp2f(-CAREFUL<TT>);
+            const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll 1
             for (int i = 0; i < count * BK; ++i) {
                 const int p = slot_of(mine + stride * (i / BK)) + i % BK;
@@ -416,6 +422,7 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
     float top = s_m[0][col];
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) top = fmaxf(top, s_m[w][col]);
+    top += JOINED;
     const float share = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
     const bool direct = sp.parts == 1;
     const int orow = threadIdx.x >> 4, piece = threadIdx.x & 15;           // 16 lanes write a row
@@ -423,6 +430,7 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
     float sum = 0.f, otop = s_m[0][orow];
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) otop = fmaxf(otop, s_m[w][orow]);
+    otop += JOINED;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) sum += s_m[w][orow] == -INFINITY ? s_l[w][orow] : s_l[w][orow] * __builtin_amdgcn_exp2f(s_m[w][orow] - otop);
     const float inv = sum != 0.f ? 1.f / sum : 0.f;
@@ -462,7 +470,7 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
     if (piece == 0 && own) {
         if (a.ml) { a.ml[cell * 32 + orow] = otop; a.ml[cell * 32 + 16 + orow] = sum; }
         if (!STEP && a.lse && direct)
-            a.lse[(int64_t)(t.q.row0 + otoken) * (c.kv_heads * group) + ohead] = otop == -INFINITY ? INFINITY : otop + BIAS<TT> + __builtin_amdgcn_logf(sum);
+            a.lse[(int64_t)(t.q.row0 + otoken) * (c.kv_heads * group) + ohead] = otop == -INFINITY ? INFINITY : otop + __builtin_amdgcn_logf(sum);
     }
 }
 
@@ -481,7 +489,7 @@ __device__ __forceinline__ void parts_of(const float* ml, int parts, int most, i
     top = fmaxf(top, dpp<0xB1>(top)); top = fmaxf(top, dpp<0x4E>(top)); top = fmaxf(top, dpp<0x141>(top)); top = fmaxf(top, dpp<0x140>(top));
     float x0, x1;
     lane_pair<16>(top, x0, x1); top = fmaxf(x0, x1);
-    lane_pair<32>(top, x0, x1); top = fmaxf(x0, x1);
+    lane_pair<32>(top, x0, x1); top = fmaxf(x0, x1) + JOINED;
     share = m == -INFINITY ? (l == l ? 0.f : l) : __builtin_amdgcn_exp2f(m - top);
     sum = rows_sum(row_allsum(m == -INFINITY ? l : l * share));
 }
@@ -498,7 +506,7 @@ __device__ __forceinline__ void put_row(const WkvPagedCall& a, const Tile& t, in
     else
         *reinterpret_cast<f32x4_t*>(dst) = f32x4_t{mean<TT>(y[0], inv), mean<TT>(y[1], inv), mean<TT>(y[2], inv), mean<TT>(y[3], inv)};
     if (!STEP && a.lse && x4 == 0)
-        a.lse[(int64_t)(t.q.row0 + token) * (a.c.kv_heads * a.c.group) + head] = top == -INFINITY ? INFINITY : top + BIAS<TT> + __builtin_amdgcn_logf(sum);
+        a.lse[(int64_t)(t.q.row0 + token) * (a.c.kv_heads * a.c.group) + head] = top == -INFINITY ? INFINITY : top + __builtin_amdgcn_logf(sum);
 }
 
 template <bool STEP> __device__ __forceinline__ Span span_of_row(const WkvPagedCall& a, const Tile& t, int row)
@@ -535,6 +543,7 @@ void wkv_paged_join_few_kernel(const WkvPagedCall a, int rows, int per_tile)
         }
 #pragma unroll
     for (int i = 0; i < FEW; ++i) if (i < sp.parts) top = fmaxf(top, m[i]);
+    top += JOINED;
 #pragma unroll
     for (int i = 0; i < FEW; ++i)
         if (i < sp.parts) {
@@ -584,7 +593,6 @@ void wkv_paged_join_kernel(const WkvPagedCall a, int per_tile)
 // Weights of a step, summed over a unit's heads and added to the slots' sums: a workgroup takes TALLY of the keys that the unit saw,
 // in the order of span().
 constexpr int HEADS = 256;           // heads of a unit whose log-sum-exps are at hand at a time
-template <class TT>
 __global__ __launch_bounds__(THREADS)
 void wkv_paged_tally_kernel(const WkvPagedCall a, int per_unit)
 {
@@ -609,7 +617,7 @@ void wkv_paged_tally_kernel(const WkvPagedCall a, int per_unit)
         for (int r = wave; r < n; r += WAVES) {
             float top, sum, share;
             parts_of(a.ml + ((int64_t)unit * a.tiles + (g0 + r) / ROWS) * a.splits * 32 + (g0 + r) % ROWS, sp.parts, a.splits, lane, top, sum, share);
-            if (lane == 0) s_lse[r] = top == -INFINITY ? INFINITY : top + BIAS<TT> + __builtin_amdgcn_logf(sum);
+            if (lane == 0) s_lse[r] = top == -INFINITY ? INFINITY : top + __builtin_amdgcn_logf(sum);
         }
         __syncthreads();
         const float* lg = a.logits + ((int64_t)unit * group + g0) * a.logit_stride;
@@ -788,7 +796,7 @@ hipError_t wkv_launch_paged_attend(const WkvPagedCall& a, int dtype, int head_di
         }
         if (e == hipSuccess && a.logits) {
             const int per_unit = (int)((wkv_paged_most_keys(a.c, 1) + TALLY - 1) / TALLY);
-            hipLaunchKernelGGL((wkv_paged_tally_kernel<TT>), dim3((unsigned)(units * per_unit)), block, 0, stream, a, per_unit);
+            hipLaunchKernelGGL(wkv_paged_tally_kernel, dim3((unsigned)(units * per_unit)), block, 0, stream, a, per_unit);
             e = hipGetLastError();
         }
         return e;

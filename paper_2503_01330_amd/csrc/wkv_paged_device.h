@@ -45,10 +45,12 @@ template <class TT> __device__ __forceinline__ void unpack2(uint32_t w, float& l
     }
 }
 
-// Weights are 2^(logit - reference), the reference being a logit that none exceeds by more than 8: sums of values up to the format's
-// largest stay finite while the weights' own sum does not exceed 1, so where values reach 2^128 every weight is times 2^-32 (a
-// sequence has at most 2^24 slots).
-template <class TT> constexpr float BIAS = __is_same(TT, TF16) ? 0.f : 32.f;
+// Weights are 2^(logit - reference), the reference being a logit (log2) that none exceeds by more than 8, so sums of 16-bit values up to 2^128 and of
+// fp32 values may leave the range of fp32 although their mean does not.  Such a sum is formed anew with every weight times
+// 2^-CAREFUL, which is a larger reference (a sequence has at most 2^24 slots); a reference that is larger from the start would cost the exponents
+// of all weights 5 bits.  Where sums of several waves or parts are joined, the common reference is JOINED above the largest.
+template <class TT> constexpr float CAREFUL = __is_same(TT, TF16) ? 0.f : 32.f;
+constexpr float JOINED = 8.f;
 
 // A row's output from its sum of weight . v.  It is a mean of values, so roundings must not take it over the format's largest number.
 template <class TT> __device__ __forceinline__ float mean(float sum, float inv)
