@@ -235,7 +235,6 @@ hipError_t wkv_launch_paged_evict(const WkvPages& c, int row_bytes, int budget, 
     constexpr int PIECE = 64;         // of 128 bytes, few units leave half the chip idle (4 x 32768 slots of 8 heads to 2048: 18.5 us, 13.5 of 64)
     const int units = c.batch * c.kv_heads, pieces = row_bytes / PIECE, list_stride = std::min(budget, c.max_slots);
     const int per_unit = 2 * pieces + 1, eights = (units + 7) / 8 * 8;
-    if ((int64_t)eights * per_unit >= 1 << 22) return hipErrorInvalidValue;       // 2^32 threads
     // (sequences of up to 4096 slots: 8 us with 4 scores a thread, 17 with 32)
     if (c.max_slots <= 4 * THREADS) hipLaunchKernelGGL((wkv_evict_select_kernel<4>), dim3(units), dim3(THREADS), 0, stream, c, budget, list_stride, recent, kept, plan, list);
     else hipLaunchKernelGGL((wkv_evict_select_kernel<32>), dim3(units), dim3(THREADS), 0, stream, c, budget, list_stride, recent, kept, plan, list);

@@ -446,43 +446,38 @@ void wkv_paged_colsum_kernel(const WkvPagedCall a, int by_unit, int64_t fast, in
         r_lo += row_part * each;
         r_hi = min(r_hi, r_lo + each);
     }
-    // The lane's rows of a load and its token and head, moved on by QROWS rows from one tile to the next; those of the thread's
-    // log-sum-exp (threads 0 .. 63).
-    struct Place { int row, token, head; };
-    const int step_t = QROWS / group, step_h = QROWS % group;
-    auto place = [&](int row) { Place p = {row, row / group, 0}; p.head = row - p.token * group; return p; };
-    auto move = [&](Place& p) {
-        p.row += QROWS;
-        p.token += step_t;
-        p.head += step_h;
-        if (p.head >= group) { p.head -= group; ++p.token; }
-    };
+    // Where the lane's rows of a load are: from one tile to the next a fixed distance on, where the group's size divides QROWS
+    const bool even = QROWS % group == 0;
     const int lrow = lane / CHUNKS, piece = lane % CHUNKS;
-    Place at[LOADS], mine = place(r_lo + (threadIdx.x & 63));
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) at[i] = place(r_lo + (i * WAVES + wave) * RPL + lrow);
-    const int last_t = t.q.n - 1, last_h = group - 1;
     const char* qh = a.q + t.q.row0 * a.q_bytes + (int64_t)t.h * group * a.q_head;
-    auto load = [&](uint32_t q) {
+    auto row_at = [&](int row) {                             // (rows behind the last one: that one again, with a weight of 0)
+        const int r = min(row, t.rows - 1), token = r / group;
+        return qh + token * a.q_bytes + (r - token * group) * a.q_head;
+    };
+    const char* at[LOADS];
+    if (r_lo < r_hi)
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) at[i] = row_at(r_lo + (i * WAVES + wave) * RPL + lrow);
+    auto load = [&](uint32_t q, int r0) {
+        const bool known = even && r0 + QROWS <= t.rows;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int r = (i * WAVES + wave) * RPL + lrow;
-            const bool ok = at[i].row < t.rows;              // (rows behind the last one: that one again, with a weight of 0)
-            const char* src = qh + (ok ? at[i].token : last_t) * a.q_bytes + (ok ? at[i].head : last_h) * a.q_head;
-            load_lds(src + ((piece ^ Block<D, 32>::turn_k(r)) * 16), q + (i * WAVES + wave) * 1024);
-            move(at[i]);
+            if (!known) at[i] = row_at(r0 + r);
+            load_lds(at[i] + ((piece ^ Block<D, 32>::turn_k(r)) * 16), q + (i * WAVES + wave) * 1024);
+            at[i] += QROWS / group * a.q_bytes;
         }
     };
     float lse = INFINITY;
     int pos = -1;
-    auto load_row = [&] {
+    auto load_row = [&](int r0) {
         lse = INFINITY;
         pos = -1;
-        if (threadIdx.x < QROWS && mine.row < t.rows) {
-            lse = a.lse[(int64_t)(t.q.row0 + mine.token) * (c.kv_heads * group) + t.h * group + mine.head];
-            pos = t.pos0 + mine.token;
+        const int row = r0 + threadIdx.x, token = row / group;
+        if (threadIdx.x < QROWS && row < t.rows) {
+            lse = a.lse[(int64_t)(t.q.row0 + token) * (c.kv_heads * group) + t.h * group + row - token * group];
+            pos = t.pos0 + token;
         }
-        move(mine);
     };
     auto keep_row = [&](int x) {
         if (threadIdx.x < QROWS) { s_lse[x][threadIdx.x] = lse; s_pos[x][threadIdx.x] = pos; }
@@ -530,15 +525,15 @@ void wkv_paged_colsum_kernel(const WkvPagedCall a, int by_unit, int64_t fast, in
         asm volatile("" ::: "memory");
     };
     if (r_lo < r_hi) {
-        load(q0);
-        load_row();
+        load(q0, r_lo);
+        load_row(r_lo);
         keep_row(0);
         for (int r0 = r_lo, x = 0; r0 < r_hi; r0 += QROWS, x ^= 1) {
             arrive();
             const bool more = r0 + QROWS < r_hi;
             if (more) {
-                load(q0 + (x ^ 1) * BYTES);
-                load_row();
+                load(q0 + (x ^ 1) * BYTES, r0 + QROWS);
+                load_row(r0 + QROWS);
             }
             use(q0 + x * BYTES, x, r0);
             if (more) keep_row(x ^ 1);

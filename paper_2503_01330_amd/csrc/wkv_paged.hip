@@ -9,7 +9,8 @@
 //                    wants (O^T = V^T P^T), so the weights never leave their lane; the values' operand is a transposition of 16-bit
 //                    words within a lane.  The waves' sums are joined through LDS.
 //   wkv_paged_join   the parts of a row joined (join_few: of few parts).
-//   wkv_paged_tally  the weights of a step summed for every slot, from the logits that wkv_paged_rows left and the parts' sums.
+//                    Behind the joins in the same launch, the weights of a step are summed for every slot, from the logits that
+//                    wkv_paged_rows left and the parts' sums (tally).
 //   wkv_paged_sums   the weights of a prefill's rows summed for every slot, from the rows' log-sum-exps.
 // New K and V rows go into their pages on the way: a call reads its own tokens from where they are, so nothing waits for that.
 //
@@ -494,110 +495,13 @@ __device__ __forceinline__ void parts_of(const float* ml, int parts, int most, i
     sum = rows_sum(row_allsum(m == -INFINITY ? l : l * share));
 }
 
-// The joined row's output, and its log-sum-exp for a prefill whose weights are summed.
-template <class TT, bool STEP>
-__device__ __forceinline__ void put_row(const WkvPagedCall& a, const Tile& t, int row, int x4, f32x4_t y, float top, float sum)
-{
-    const float inv = sum != 0.f ? 1.f / sum : 0.f;
-    const int token = STEP ? 0 : row / a.c.group, head = t.h * a.c.group + row - token * a.c.group;
-    char* dst = a.out + (t.q.row0 + token) * a.out_bytes + head * a.out_head + x4 * (4 * TT::BYTES);
-    if constexpr (TT::BYTES == 2)
-        *reinterpret_cast<uint2*>(dst) = make_uint2(pack2<TT>(mean<TT>(y[0], inv), mean<TT>(y[1], inv)), pack2<TT>(mean<TT>(y[2], inv), mean<TT>(y[3], inv)));
-    else
-        *reinterpret_cast<f32x4_t*>(dst) = f32x4_t{mean<TT>(y[0], inv), mean<TT>(y[1], inv), mean<TT>(y[2], inv), mean<TT>(y[3], inv)};
-    if (!STEP && a.lse && x4 == 0)
-        a.lse[(int64_t)(t.q.row0 + token) * (a.c.kv_heads * a.c.group) + head] = top == -INFINITY ? INFINITY : top + __builtin_amdgcn_logf(sum);
-}
-
-template <bool STEP> __device__ __forceinline__ Span span_of_row(const WkvPagedCall& a, const Tile& t, int row)
-{
-    if constexpr (STEP) return span(a, t.pos0, t.pos0);
-    const int t0 = row & -a.tile_rows, t1 = min(t.rows, t0 + a.tile_rows);          // (the keys were cut into parts for that tile)
-    return span(a, t.pos0 + t0 / a.c.group, t.pos0 + (t1 - 1) / a.c.group);
-}
-
-// Row x of all cells (per_tile of each): a workgroup joins SETS rows of a few parts, D / 4 lanes each.
-constexpr int FEW = 4;
-template <class TT, int D, bool STEP>
-__global__ __launch_bounds__(THREADS)
-void wkv_paged_join_few_kernel(const WkvPagedCall a, int rows, int per_tile)
-{
-    constexpr int LANES = D / 4, SETS = THREADS / LANES;
-    const int x = blockIdx.x * SETS + threadIdx.x / LANES, x4 = threadIdx.x % LANES;
-    if (x >= rows) return;
-    const int at = x % per_tile, cell = x / per_tile, unit = cell / a.tiles, row = (cell - unit * a.tiles) * ROWS + at;
-    Tile t;
-    if (!unit_of<STEP>(a, unit, row, t)) return;
-    const Span sp = span_of_row<STEP>(a, t, row);
-    if (sp.parts == 1) return;
-    const float* ml = a.ml + (int64_t)cell * a.splits * 32 + at;
-    const float* src = a.part + ((int64_t)cell * a.splits * ROWS + at) * D + x4 * 4;
-    float m[FEW], l[FEW], top = -INFINITY, sum = 0.f;
-    f32x4_t v[FEW], y = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < FEW; ++i)
-        if (i < sp.parts) {
-            m[i] = ml[i * 32];
-            l[i] = ml[i * 32 + 16];
-            v[i] = *reinterpret_cast<const f32x4_t*>(src + (int64_t)i * ROWS * D);
-        }
-#pragma unroll
-    for (int i = 0; i < FEW; ++i) if (i < sp.parts) top = fmaxf(top, m[i]);
-    top += JOINED;
-#pragma unroll
-    for (int i = 0; i < FEW; ++i)
-        if (i < sp.parts) {
-            const float f = m[i] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[i] - top);
-            sum += f * l[i];
-            y += f * v[i];
-        }
-    put_row<TT, STEP>(a, t, row, x4, y, top, sum);
-}
-
-// The same for up to 64 parts, a workgroup a row: its waves' lanes sum parts side by side.
-template <class TT, int D, bool STEP>
-__global__ __launch_bounds__(THREADS, 4)
-void wkv_paged_join_kernel(const WkvPagedCall a, int per_tile)
-{
-    constexpr int LANES = D / 4, SETS = THREADS / LANES, DEEP = 64 / SETS;         // parts side by side, one after the other
-    __shared__ f32x4_t s_x[SETS][LANES];
-    const int lane = threadIdx.x & 63;
-    const int at = blockIdx.x % per_tile, cell = blockIdx.x / per_tile, unit = cell / a.tiles, row = (cell - unit * a.tiles) * ROWS + at;
-    const float* ml = a.ml + (int64_t)cell * a.splits * 32 + at;
-    const int set = threadIdx.x / LANES, x4 = threadIdx.x % LANES;
-    const float* src = a.part + ((int64_t)cell * a.splits * ROWS + at) * D + x4 * 4;
-    f32x4_t x[DEEP];
-#pragma unroll
-    for (int i = 0; i < DEEP; ++i)
-        if (i * SETS + set < a.splits) x[i] = *reinterpret_cast<const f32x4_t*>(src + (int64_t)(i * SETS + set) * ROWS * D);
-    Tile t;
-    if (!unit_of<STEP>(a, unit, row, t)) return;
-    const Span sp = span_of_row<STEP>(a, t, row);
-    if (sp.parts == 1) return;
-    float top, sum, share;
-    parts_of(ml, sp.parts, a.splits, lane, top, sum, share);
-    f32x4_t y = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < DEEP; ++i) {
-        const float f = __shfl(share, i * SETS + set);
-        if (i * SETS + set < sp.parts) y += f * x[i];
-    }
-    s_x[set][x4] = y;
-    __syncthreads();
-    if (set > 0) return;
-#pragma unroll
-    for (int i = 1; i < SETS; ++i) y += s_x[i][x4];
-    put_row<TT, STEP>(a, t, row, x4, y, top, sum);
-}
-
 // Weights of a step, summed over a unit's heads and added to the slots' sums: a workgroup takes TALLY of the keys that the unit saw,
 // in the order of span().
 constexpr int HEADS = 256;           // heads of a unit whose log-sum-exps are at hand at a time
-__global__ __launch_bounds__(THREADS)
-void wkv_paged_tally_kernel(const WkvPagedCall a, int per_unit)
+__device__ __forceinline__ void tally(const WkvPagedCall& a, int block, int per_unit)
 {
     __shared__ float s_lse[HEADS];
-    const int unit = blockIdx.x / per_unit, first = blockIdx.x % per_unit * TALLY;
+    const int unit = block / per_unit, first = block % per_unit * TALLY;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = a.c.group;
     Tile t;
     unit_of<true>(a, unit, 0, t);
@@ -634,6 +538,110 @@ void wkv_paged_tally_kernel(const WkvPagedCall a, int per_unit)
         if (at[i] == t.pos0 && a.k_new) sc[at[i]] = w[i];
         else sc[at[i]] += w[i];
     }
+}
+
+// The joined row's output, and its log-sum-exp for a prefill whose weights are summed.
+template <class TT, bool STEP>
+__device__ __forceinline__ void put_row(const WkvPagedCall& a, const Tile& t, int row, int x4, f32x4_t y, float top, float sum)
+{
+    const float inv = sum != 0.f ? 1.f / sum : 0.f;
+    const int token = STEP ? 0 : row / a.c.group, head = t.h * a.c.group + row - token * a.c.group;
+    char* dst = a.out + (t.q.row0 + token) * a.out_bytes + head * a.out_head + x4 * (4 * TT::BYTES);
+    if constexpr (TT::BYTES == 2)
+        *reinterpret_cast<uint2*>(dst) = make_uint2(pack2<TT>(mean<TT>(y[0], inv), mean<TT>(y[1], inv)), pack2<TT>(mean<TT>(y[2], inv), mean<TT>(y[3], inv)));
+    else
+        *reinterpret_cast<f32x4_t*>(dst) = f32x4_t{mean<TT>(y[0], inv), mean<TT>(y[1], inv), mean<TT>(y[2], inv), mean<TT>(y[3], inv)};
+    if (!STEP && a.lse && x4 == 0)
+        a.lse[(int64_t)(t.q.row0 + token) * (a.c.kv_heads * a.c.group) + head] = top == -INFINITY ? INFINITY : top + __builtin_amdgcn_logf(sum);
+}
+
+template <bool STEP> __device__ __forceinline__ Span span_of_row(const WkvPagedCall& a, const Tile& t, int row)
+{
+    if constexpr (STEP) return span(a, t.pos0, t.pos0);
+    const int t0 = row & -a.tile_rows, t1 = min(t.rows, t0 + a.tile_rows);          // (the keys were cut into parts for that tile)
+    return span(a, t.pos0 + t0 / a.c.group, t.pos0 + (t1 - 1) / a.c.group);
+}
+
+// Workgroups 0 .. joins - 1 join the parts of rows; behind them, for a step whose weights are summed, they tally.
+//
+// Row x of all cells (per_tile of each): a workgroup joins SETS rows of a few parts, D / 4 lanes each.
+constexpr int FEW = 4;
+template <class TT, int D, bool STEP>
+__global__ __launch_bounds__(THREADS)
+void wkv_paged_join_few_kernel(const WkvPagedCall a, int joins, int rows, int per_tile, int per_unit)
+{
+    if constexpr (STEP) {
+        if ((int)blockIdx.x >= joins) return tally(a, blockIdx.x - joins, per_unit);
+    }
+    constexpr int LANES = D / 4, SETS = THREADS / LANES;
+    const int x = blockIdx.x * SETS + threadIdx.x / LANES, x4 = threadIdx.x % LANES;
+    if (x >= rows) return;
+    const int at = x % per_tile, cell = x / per_tile, unit = cell / a.tiles, row = (cell - unit * a.tiles) * ROWS + at;
+    Tile t;
+    if (!unit_of<STEP>(a, unit, row, t)) return;
+    const Span sp = span_of_row<STEP>(a, t, row);
+    if (sp.parts == 1) return;
+    const float* ml = a.ml + (int64_t)cell * a.splits * 32 + at;
+    const float* src = a.part + ((int64_t)cell * a.splits * ROWS + at) * D + x4 * 4;
+    float m[FEW], l[FEW], top = -INFINITY, sum = 0.f;
+    f32x4_t v[FEW], y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < FEW; ++i)
+        if (i < sp.parts) {
+            m[i] = ml[i * 32];
+            l[i] = ml[i * 32 + 16];
+            v[i] = *reinterpret_cast<const f32x4_t*>(src + (int64_t)i * ROWS * D);
+        }
+#pragma unroll
+    for (int i = 0; i < FEW; ++i) if (i < sp.parts) top = fmaxf(top, m[i]);
+    top += JOINED;
+#pragma unroll
+    for (int i = 0; i < FEW; ++i)
+        if (i < sp.parts) {
+            const float f = m[i] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[i] - top);
+            sum += f * l[i];
+            y += f * v[i];
+        }
+    put_row<TT, STEP>(a, t, row, x4, y, top, sum);
+}
+
+// The same for up to 64 parts, a workgroup a row: its waves' lanes sum parts side by side.
+template <class TT, int D, bool STEP>
+__global__ __launch_bounds__(THREADS, 4)
+void wkv_paged_join_kernel(const WkvPagedCall a, int joins, int per_tile, int per_unit)
+{
+    if constexpr (STEP) {
+        if ((int)blockIdx.x >= joins) return tally(a, blockIdx.x - joins, per_unit);
+    }
+    constexpr int LANES = D / 4, SETS = THREADS / LANES, DEEP = 64 / SETS;         // parts side by side, one after the other
+    __shared__ f32x4_t s_x[SETS][LANES];
+    const int lane = threadIdx.x & 63;
+    const int at = blockIdx.x % per_tile, cell = blockIdx.x / per_tile, unit = cell / a.tiles, row = (cell - unit * a.tiles) * ROWS + at;
+    const float* ml = a.ml + (int64_t)cell * a.splits * 32 + at;
+    const int set = threadIdx.x / LANES, x4 = threadIdx.x % LANES;
+    const float* src = a.part + ((int64_t)cell * a.splits * ROWS + at) * D + x4 * 4;
+    f32x4_t x[DEEP];
+#pragma unroll
+    for (int i = 0; i < DEEP; ++i)
+        if (i * SETS + set < a.splits) x[i] = *reinterpret_cast<const f32x4_t*>(src + (int64_t)(i * SETS + set) * ROWS * D);
+    Tile t;
+    if (!unit_of<STEP>(a, unit, row, t)) return;
+    const Span sp = span_of_row<STEP>(a, t, row);
+    if (sp.parts == 1) return;
+    float top, sum, share;
+    parts_of(ml, sp.parts, a.splits, lane, top, sum, share);
+    f32x4_t y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < DEEP; ++i) {
+        const float f = __shfl(share, i * SETS + set);
+        if (i * SETS + set < sp.parts) y += f * x[i];
+    }
+    s_x[set][x4] = y;
+    __syncthreads();
+    if (set > 0) return;
+#pragma unroll
+    for (int i = 1; i < SETS; ++i) y += s_x[i][x4];
+    put_row<TT, STEP>(a, t, row, x4, y, top, sum);
 }
 
 // ---------------------------------------------------------------- weights of a prefill's rows, summed for every slot
@@ -781,22 +789,17 @@ hipError_t wkv_launch_paged_attend(const WkvPagedCall& a, int dtype, int head_di
         else if (!a.logits) hipLaunchKernelGGL((wkv_paged_rows_kernel<TT, D, true, false, false>), grid, block, 0, stream, a);
         else hipLaunchKernelGGL((wkv_paged_rows_kernel<TT, D, true, false, true>), grid, block, 0, stream, a);
         if (e == hipSuccess) e = hipGetLastError();
-        if (e == hipSuccess && a.splits > 1) {
+        if (e == hipSuccess && (a.splits > 1 || a.logits)) {
             const int per_tile = (int)std::min<int64_t>(ROWS, (int64_t)a.max_new * a.c.group);
-            const int rows = (int)(units * a.tiles * per_tile);
-            if (a.splits <= FEW) {
-                const dim3 few((unsigned)((rows + THREADS * 4 / D - 1) / (THREADS * 4 / D)));
-                if (a.starts) hipLaunchKernelGGL((wkv_paged_join_few_kernel<TT, D, false>), few, block, 0, stream, a, rows, per_tile);
-                else hipLaunchKernelGGL((wkv_paged_join_few_kernel<TT, D, true>), few, block, 0, stream, a, rows, per_tile);
-            } else {
-                if (a.starts) hipLaunchKernelGGL((wkv_paged_join_kernel<TT, D, false>), dim3(rows), block, 0, stream, a, per_tile);
-                else hipLaunchKernelGGL((wkv_paged_join_kernel<TT, D, true>), dim3(rows), block, 0, stream, a, per_tile);
-            }
-            e = hipGetLastError();
-        }
-        if (e == hipSuccess && a.logits) {
-            const int per_unit = (int)((wkv_paged_most_keys(a.c, 1) + TALLY - 1) / TALLY);
-            hipLaunchKernelGGL(wkv_paged_tally_kernel, dim3((unsigned)(units * per_unit)), block, 0, stream, a, per_unit);
+            const int rows = a.splits > 1 ? (int)(units * a.tiles * per_tile) : 0;
+            const int per_unit = a.logits ? (int)((wkv_paged_most_keys(a.c, 1) + TALLY - 1) / TALLY) : 0;
+            const bool few = a.splits <= FEW;
+            const int sets = few ? THREADS * 4 / D : 1, joins = (rows + sets - 1) / sets;
+            const dim3 all((unsigned)(joins + units * per_unit));
+            if (few && a.starts) hipLaunchKernelGGL((wkv_paged_join_few_kernel<TT, D, false>), all, block, 0, stream, a, joins, rows, per_tile, 1);
+            else if (few) hipLaunchKernelGGL((wkv_paged_join_few_kernel<TT, D, true>), all, block, 0, stream, a, joins, rows, per_tile, per_unit);
+            else if (a.starts) hipLaunchKernelGGL((wkv_paged_join_kernel<TT, D, false>), all, block, 0, stream, a, joins, per_tile, 1);
+            else hipLaunchKernelGGL((wkv_paged_join_kernel<TT, D, true>), all, block, 0, stream, a, joins, per_tile, per_unit);
             e = hipGetLastError();
         }
         return e;

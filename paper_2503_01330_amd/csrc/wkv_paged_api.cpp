@@ -157,7 +157,7 @@ int attend(const wkv_paged* p, const wkv_paged_rows* r, const int32_t* starts, i
     const int64_t units = (int64_t)p->batch * p->kv_heads;
     if (units * a.tiles * a.splits >= 1 << 24)
         return fail(WKV_ESIZE, "%lld row tiles in %d parts: a launch holds fewer than 2^32 threads", (long long)(units * a.tiles), a.splits);
-    if (a.logits && units * ((a.c.max_slots + 1023) / 1024) >= 1 << 23)
+    if (a.logits && units * ((a.c.max_slots + 1023) / 1024) >= (1 << 23) - (1 << 16))
         return fail(WKV_ESIZE, "%lld units of %d slots: a launch holds fewer than 2^32 threads", (long long)units, a.c.max_slots);
     hipError_t e = wkv_launch_paged_attend(a, p->dtype, p->head_dim, stream);
     if (e == hipSuccess && !step && p->scores) e = wkv_launch_paged_sums(a, p->dtype, p->head_dim, stream);
@@ -204,6 +204,8 @@ int wkv_paged_evict(const wkv_paged* c, int budget, int recent_window, int32_t* 
     if (budget < 1 || recent_window < 1 || (int64_t)c->n_sink + recent_window > budget)
         return fail(WKV_EINVAL, "1 <= recent_window and n_sink + recent_window <= budget are wanted: %d, %d, %d", recent_window, c->n_sink, budget);
     const WkvPages p = pages_of(*c);
+    if ((int64_t)c->batch * c->kv_heads * (c->head_dim * elem_bytes(c->dtype) / 32 + 1) >= 1 << 22)
+        return fail(WKV_ESIZE, "%d units: a launch holds fewer than 2^32 threads", c->batch * c->kv_heads);
     // (a budget that no sequence can exceed leaves all of them as they are)
     rc = check_work(workspace, workspace_bytes, evict_bytes(*c, std::min(budget, p.max_slots)));
     if (rc != WKV_OK) return rc;
