@@ -204,9 +204,6 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
     auto use = [&](uint32_t kb, uint32_t vb, int pos, const int (&pages)[NG]) __attribute__((always_inline)) {
         if (pos > p_hi) return;                                            // (the wave's rows are all before it)
         asm("" : "+v"(k_at), "+v"(v_at));                 // (addresses made of these are not kept in registers from block to block)
-#ifdef PRIO
-        __builtin_amdgcn_s_setprio(1);
-#endif
         f32x16_t s[NB];
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
@@ -217,9 +214,6 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
                 s[b] = mfma32<TT>(k, q[i], s[b]);
             }
         }
-#ifdef PRIO
-        __builtin_amdgcn_s_setprio(0);
-#endif
         const bool full = all_there(pages) && pos + BK - 1 <= p_lo && (pos > p_hi - window || pos + BK <= c.n_sink);
         if (!full) {
 #pragma unroll
