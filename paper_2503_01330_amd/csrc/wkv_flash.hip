@@ -151,7 +151,7 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
         const bool inside = all_there(pages) && pos + BK - 1 <= t_hi && (pos > t_lo - window || pos + BK <= c.n_sink);
         const uint32_t kl = kb + wave * 1024, vl = vb + wave * 1024;
         int ln = threadIdx.x & 63;                        // (and what follows from it: not kept from block to block)
-        asm volatile("" : "+v"(ln));
+        if constexpr (D > 128) asm volatile("" : "+v"(ln));
         const int lrow = ln / B::CHUNKS, lpiece = ln % B::CHUNKS;
         // load i: its first row, the lane's, the page (in narrow rows the waves' loads are of two stretches of 16 slots)
         auto first = [&](int i) { return (i * WAVES + wave) * B::RPL; };
@@ -203,7 +203,7 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
 
     auto use = [&](uint32_t kb, uint32_t vb, int pos, const int (&pages)[NG]) __attribute__((always_inline)) {
         if (pos > p_hi) return;                                            // (the wave's rows are all before it)
-        asm("" : "+v"(k_at), "+v"(v_at));                 // (addresses made of these are not kept in registers from block to block)
+        if constexpr (D > 128) asm("" : "+v"(k_at), "+v"(v_at));          // (addresses made of these are not kept in registers from block to block)
         f32x16_t s[NB];
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
