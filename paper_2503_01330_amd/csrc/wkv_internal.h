@@ -152,9 +152,9 @@ hipError_t wkv_launch_paged_colsum(const WkvPagedCall& a, int dtype, int head_di
 hipError_t wkv_launch_paged_flash(const WkvPagedCall& a, int dtype, int head_dim, hipStream_t stream);
 // Most keys that a query sees, or the queries of new_tokens tokens next to each other.
 int64_t wkv_paged_most_keys(const WkvPages& c, int64_t new_tokens);
-// Which kernel a call of `rows` rows a unit at most takes, and into how many parts it cuts a tile's keys, of which there are
-// most_keys at most: fills many, tiles, splits, tile_rows, block and least.
-void wkv_paged_shape(WkvPagedCall& a, int64_t units, int64_t rows, int64_t most_keys, int dtype, int head_dim);
+// Which kernel a call of `rows` rows a unit at most takes (a step: always the one for few), and into how many parts it cuts a tile's keys,
+// of which there are most_keys at most: fills many, tiles, splits, tile_rows, block, least and order.
+void wkv_paged_shape(WkvPagedCall& a, int64_t units, int64_t rows, int64_t most_keys, int dtype, int head_dim, bool step);
 
 // plan: [batch][2] lengths before and after; list: [unit][budget] slots that are left, ascending
 hipError_t wkv_launch_paged_evict(const WkvPages& c, int row_bytes, int budget, int recent, int32_t* new_lens, float* new_scores,

@@ -740,13 +740,14 @@ int64_t wkv_paged_most_keys(const WkvPages& c, int64_t new_tokens)
     return c.window > 0 ? std::min<int64_t>(c.max_slots, (int64_t)c.window + c.n_sink + new_tokens + 128) : c.max_slots;
 }
 
-void wkv_paged_shape(WkvPagedCall& a, int64_t units, int64_t rows, int64_t most, int dtype, int head_dim)
+void wkv_paged_shape(WkvPagedCall& a, int64_t units, int64_t rows, int64_t most, int dtype, int head_dim, bool step)
 {
     a.tiles = (int)((rows + ROWS - 1) / ROWS);
     // The kernel for many rows is ahead from about 32 rows on (2000 slots: 20 rows 19.4 us against 15.6 of the other, 48 rows 19.4 | 20.0; 80 rows onto 8000
     // slots 23 | 43), but not for short prompts that leave the chip half empty either way (77 tokens of 32 K/V heads 15.2 | 12.5, 256 tokens of 8 with
-    // four query heads each 17.9 | 16.0; 4 x 128 of these 15.8 | 20.7).
-    a.many = dtype != WKV_FP32 && rows > 32 && (units * a.tiles > 512 || a.c.max_slots > 256);
+    // four query heads each 17.9 | 16.0; 4 x 128 of these 15.8 | 20.7).  Steps, of however many heads, are the other's: it has their rows without `starts`
+    // and keeps their logits.
+    a.many = !step && dtype != WKV_FP32 && rows > 32 && (units * a.tiles > 512 || a.c.max_slots > 256);
     a.tile_rows = a.many ? 128 : ROWS;
     const int64_t groups = units * ((rows + a.tile_rows - 1) / a.tile_rows);
     auto over = [&](int64_t n) { return (n + groups - 1) / groups; };
@@ -768,7 +769,7 @@ void wkv_paged_shape(WkvPagedCall& a, int64_t units, int64_t rows, int64_t most,
     // 1 x 4096, 32 K/V heads 19.1 | 21.5 | 21.9 | 23.9, 8 x 8192 48.8 | 50.8 | 48.6 | 55.7, 4 x 32768 95.8 | 98.0 | 92.7.
     a.splits = parts(std::max(over(256), std::min(over(768), most / 1024)), (int64_t)a.block * a.least);
     // More workgroups than run at once: the longest sequences first (64 ragged sequences, 1024 workgroups: 157 -> 148 us).
-    a.order = a.c.batch > 1 && groups * a.splits > 768;
+    a.order = step && a.c.batch > 1 && groups * a.splits > 768;
 }
 
 hipError_t wkv_launch_paged_attend(const WkvPagedCall& a, int dtype, int head_dim, hipStream_t stream)

@@ -92,7 +92,7 @@ Layout layout(const wkv_paged& p, bool scores, int n_tokens, int max_new, bool s
     const int64_t rows = (int64_t)max_new * c.group;
     l.shape.c = c;
     l.shape.max_new = max_new;
-    wkv_paged_shape(l.shape, units, rows, wkv_paged_most_keys(c, std::min(max_new, 128 / c.group + 2)), p.dtype, p.head_dim);
+    wkv_paged_shape(l.shape, units, rows, wkv_paged_most_keys(c, std::min(max_new, 128 / c.group + 2)), p.dtype, p.head_dim, step);
     auto take = [&](size_t bytes) { const size_t at = l.total; l.total += (bytes + 255) / 256 * 256; return at; };
     const int splits = l.shape.splits;
     const size_t cells = (size_t)units * l.shape.tiles * splits;

@@ -365,6 +365,14 @@ def test_many_heads_to_a_kv_head():
     run(Paged(55, [70, 3], [5, 3], heads=300, kv_heads=1, d=64, scores=True))
 
 
+@pytest.mark.parametrize("dtype,d,heads,kv_heads", [("fp16", 64, 71, 1), ("bf16", 128, 66, 2), ("bf16", 256, 33, 1), ("fp32", 128, 48, 1)])
+@pytest.mark.parametrize("scores", [False, True])
+def test_steps_of_many_heads_to_a_kv_head(dtype, d, heads, kv_heads, scores):
+    """More rows a unit than short chunks have, onto sequences long enough for the kernel that takes longer chunks."""
+    run(Paged(56, [700, 3, 0, 290], heads=heads, kv_heads=kv_heads, d=d, dtype=dtype, page=32, scores=scores))
+    run(Paged(57, [700, 3, 0, 290], heads=heads, kv_heads=kv_heads, d=d, dtype=dtype, window=99, sink=5, scores=scores))
+
+
 @pytest.mark.parametrize("dtype,d", [("fp16", 64), ("bf16", 128), ("bf16", 256), ("fp32", 128)])
 def test_short_chunks_onto_long_sequences(dtype, d):
     """The keys are cut into parts, few and many, for both kernels."""
