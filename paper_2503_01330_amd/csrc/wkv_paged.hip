@@ -91,7 +91,7 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
         __shared__ __attribute__((aligned(16))) int s_len[THREADS];
         __shared__ int s_mine;
         const int place = unit / c.kv_heads, base = place / THREADS * THREADS, n = min(THREADS, c.batch - base);
-        const int len = (int)threadIdx.x < n ? c.lens[base + threadIdx.x] : -1;
+        const int len = (int)threadIdx.x < n ? max(c.lens[base + threadIdx.x], 0) : -1;       // (places behind the last sequence come last)
         s_len[threadIdx.x] = len;
         __syncthreads();
         int rank = 0;

@@ -360,6 +360,14 @@ def test_steps_of_many_sequences(dtype, d, scores):
     run(Paged(53, lens, heads=3, kv_heads=3, d=64, dtype=dtype, scores=scores))
 
 
+def test_lengths_below_zero_among_many_sequences():
+    """Sequences in order of their lengths, their number no multiple of 4: lengths below 0 count as 0."""
+    p = Paged(67, [n % 50 for n in range(129)] + [0], heads=8, kv_heads=8, d=64, scores=True)
+    x = p.device()
+    x["lens"].copy_(torch.tensor([n if n else -2 ** 31 + b for b, n in enumerate(p.lens)], dtype=torch.int32))
+    run(p, x=x)
+
+
 def test_many_heads_to_a_kv_head():
     run(Paged(54, [70, 3], heads=300, kv_heads=1, d=64, scores=True))
     run(Paged(55, [70, 3], [5, 3], heads=300, kv_heads=1, d=64, scores=True))
