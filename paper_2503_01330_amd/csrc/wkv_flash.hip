@@ -272,11 +272,11 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
         }
     };
 
-    // Every wave has waited for its own loads of a block when it comes to the barrier, and has read all of the block before: after it
+    // Every wave has waited for its own loads of a block when it comes to the barrier, and for what it read of the block before: after it
     // the block is whole, and the other buffer is free for the next.
     auto arrive = [&] {
         asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_waitcnt(0x0F70);               // vmcnt(0), in a form that the compiler counts by
+        __builtin_amdgcn_s_waitcnt(0x0070);               // vmcnt(0) lgkmcnt(0), in a form that the compiler counts by
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
