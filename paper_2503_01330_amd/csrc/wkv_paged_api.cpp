@@ -74,7 +74,8 @@ WkvPages pages_of(const wkv_paged& p)
     c.n_pages = p.n_pages; c.max_pages = p.max_pages;
     c.max_slots = p.max_pages * p.page_size;
     if (p.scores) c.max_slots = (int)std::min<int64_t>(c.max_slots, p.score_stride);
-    c.window = p.window; c.n_sink = p.n_sink;
+    c.window = std::min(p.window, 1 << 25);          // (twice the most slots: what a position before slot 0 is further back stays in 32 bits)
+    c.n_sink = p.n_sink;
     return c;
 }
 

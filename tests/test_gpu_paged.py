@@ -496,3 +496,15 @@ def test_the_same_call_gives_the_same_bits():
             torch.cuda.synchronize()
             got.append((x["out"], x["scores"], x["k"]))
         assert all(paged.same(a, b) for a, b in zip(*got))
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "fp32"])
+def test_the_largest_window(dtype):
+    """A window of 2^31 - 1 is none, also for tokens that have no slot (a chunk longer than its sequence)."""
+    p = Paged(68, [20, 300], [20, 260], heads=4, kv_heads=2, d=64, dtype=dtype, window=2 ** 31 - 1, sink=2, scores=True, extra_rows=5)
+    x = p.device()
+    p.lens, p.new = [13, 300], [20, 260]                     # seven rows of the first sequence before its slot 0
+    x["lens"].copy_(torch.tensor(p.lens, dtype=torch.int32))
+    run(p, x=x)
+    p = Paged(69, [20, 300], heads=4, kv_heads=2, d=64, dtype=dtype, window=2 ** 31 - 1, sink=2 ** 31 - 1, scores=True)
+    run(p)
