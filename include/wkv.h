@@ -337,7 +337,7 @@ int wkv_paged_step(const wkv_paged* c, const wkv_paged_rows* rows, void* workspa
  * tokens of sequence b, in slots lens[b]-n .. lens[b]-1.  Appends k and v, attends, and with scores adds the weights, all queries' and heads' of the group together (appended slots' sums start with this).
  *   starts  : DEVICE int32 [batch+1], not decreasing; rows behind starts[batch] are left as they are
  *   n_tokens: tokens that the rows have; max_new: at least the longest chunk (longer ones are cut to it), at
- *             most n_tokens.  A chunk longer than its sequence's lens[b]: its first rows have no slot; they see nothing.
+ *             most n_tokens and 2^24; n_tokens*heads is at most 2^30.  A chunk longer than its sequence's lens[b]: its first rows have no slot; they see nothing.
  * Asynchronous as wkv_paged_step.  How the work is shared out depends on the sizes (not on lens), and so do last bits;
  * the same call gives the same bits every time.
  */

@@ -45,6 +45,14 @@ int check_shape(const wkv_paged& c)
     return WKV_OK;
 }
 
+// A chunk's sizes: rows and their bytes are counted in 32 bits per unit.
+int check_chunk(const wkv_paged& c, int n_tokens, int max_new)
+{
+    if (max_new > 1 << 24) return fail(WKV_ESIZE, "max_new %d exceeds 2^24, the most slots of a sequence", max_new);
+    if ((int64_t)n_tokens * c.heads > 1 << 30) return fail(WKV_ESIZE, "n_tokens*heads exceeds 2^30");
+    return WKV_OK;
+}
+
 int check(const wkv_paged* c)
 {
     if (!c) return fail(WKV_EINVAL, "null argument");
@@ -138,6 +146,8 @@ int attend(const wkv_paged* p, const wkv_paged_rows* r, const int32_t* starts, i
     if ((n_tokens > 1 && r->out_stride < p->head_dim) || (p->heads > 1 && r->out_head_stride < p->head_dim))
         return fail(WKV_EINVAL, "rows of out must not overlap");
     const bool step = starts == nullptr;
+    rc = check_chunk(*p, n_tokens, max_new);
+    if (rc != WKV_OK) return rc;
     const Layout l = layout(*p, p->scores != nullptr, n_tokens, max_new, step);
     rc = check_work(workspace, workspace_bytes, l.total);
     if (rc != WKV_OK) return rc;
@@ -171,7 +181,7 @@ extern "C" {
 
 size_t wkv_paged_workspace_bytes(const wkv_paged* c, int n_tokens, int max_new)
 {
-    if (!c || check_shape(*c) != WKV_OK || n_tokens < 0 || max_new < 0 || max_new > n_tokens) return 0;
+    if (!c || check_shape(*c) != WKV_OK || n_tokens < 0 || max_new < 0 || max_new > n_tokens || check_chunk(*c, n_tokens, max_new) != WKV_OK) return 0;
     const bool scores = c->scores != nullptr;
     size_t need = std::max(layout(*c, scores, c->batch, 1, true).total, (size_t)256);
     if (max_new > 0) need = std::max(need, layout(*c, scores, n_tokens, max_new, false).total);

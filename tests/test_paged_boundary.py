@@ -149,6 +149,20 @@ def test_workspace_arithmetic():
     assert need(**long) >= (1 << 16) * 4
 
 
+def test_chunks_that_32_bits_do_not_count():
+    small = dict(heads=1, kv_heads=1, batch=1)
+    assert prefill(cache(**small), rows(), n=1 << 30, most=1 << 24) == SOUND and "workspace" in wkv.wkv_last_error()
+    assert prefill(cache(**small), rows(), n=1 << 30, most=(1 << 24) + 1) == wkv.WKV_ESIZE and "max_new" in wkv.wkv_last_error()
+    assert prefill(cache(), rows(), n=(1 << 27) + 1, most=5) == wkv.WKV_ESIZE and "n_tokens" in wkv.wkv_last_error()
+    assert wkv._lib.wkv_paged_workspace_bytes(C.byref(cache()), (1 << 27) + 1, 5) == 0
+    assert wkv._lib.wkv_paged_workspace_bytes(C.byref(cache(**small)), 1 << 30, (1 << 24) + 1) == 0
+
+
+def test_evictions_of_too_many_units_are_refused():
+    c = cache(batch=1 << 10, heads=1 << 9, kv_heads=1 << 9, n_sink=1)
+    assert evict(c, size=1 << 62) == wkv.WKV_ESIZE and "threads" in wkv.wkv_last_error()
+
+
 def test_launches_of_too_many_threads_are_refused():
     c = cache(batch=1 << 12, heads=1 << 10, kv_heads=1 << 10, page_stride=16 << 17, slot_stride=1 << 17, max_pages=1 << 10, table_stride=1 << 10)
     r = rows(q_stride=1 << 17, k_stride=1 << 17, v_stride=1 << 17, out_stride=1 << 17)
