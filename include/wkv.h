@@ -307,7 +307,8 @@ typedef struct wkv_paged {
 
 /* Rows of a call, by token and head: DEVICE, 16-byte aligned; the row of token t and head h starts at element
  * t*stride + h*head_stride.  Strides are multiples of 16 bytes and not negative (0: the same row for all; not for out); slot_stride
- * above and k_stride, v_stride are at most 2^26 bytes. */
+ * above and k_stride, v_stride are at most 2^26 bytes.  Rows of out overlap neither each other nor anything that the call reads or
+ * appends to.  All of a call's memory and its stream belong to the current device. */
 typedef struct wkv_paged_rows {
     const void* q;               /* [tokens][heads][head_dim]                                           */
     const void* k;               /* [tokens][kv_heads][head_dim], or NULL (with v): appended already    */

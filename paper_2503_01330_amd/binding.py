@@ -285,6 +285,13 @@ def _refuse(message):
     raise WkvError(WKV_EINVAL, message)
 
 
+def _ints(**kw):
+    """(ctypes keeps the lowest 32 bits of a larger number)"""
+    for name, x in kw.items():
+        if not -2 ** 31 <= x < 2 ** 31:
+            _refuse(f"{name}: {x} is no 32-bit number")
+
+
 class PagedCache:
     """A wkv_paged over torch tensors that the caller owns, and a workspace of its own.
 
@@ -297,6 +304,7 @@ class PagedCache:
     """
 
     def __init__(self, k, v, table, lens, heads, window=0, n_sink=0, scores=None, max_tokens=0, max_new=0):
+        _ints(heads=heads, window=window, n_sink=n_sink, max_tokens=max_tokens, max_new=max_new)
         if k.dim() != 4 or k.dtype not in _TORCH_STORE or v.shape != k.shape or v.dtype != k.dtype or v.stride() != k.stride():
             _refuse("k and v: [n_pages, page_size, kv_heads, head_dim] of one type and layout")
         if table.dim() != 2 or table.dtype != torch.int32 or lens.shape != table.shape[:1] or lens.dtype != torch.int32:
@@ -328,9 +336,10 @@ class PagedCache:
         need = _lib.wkv_paged_workspace_bytes(C.byref(self.c), n_tokens, max_new)
         if need == 0:
             _refuse("no workspace for these sizes: " + wkv_last_error())
-        if self._work is None or self._work.numel() < need:
-            self._kept.append(self._work)               # (work on another stream may still be using it)
-            self._work = torch.empty(need, dtype=torch.uint8, device=self.device)
+        have = 0 if self._work is None else self._work.numel()
+        if have < need:
+            self._kept.append(self._work)               # (work on another stream may still be using it, or a recorded graph)
+            self._work = torch.empty(max(need, have + have // 2), dtype=torch.uint8, device=self.device)        # (all of those: twice this one)
         self._at, self._bytes = self._work.data_ptr(), self._work.numel()
 
     def _fill(self, n, q, k, v, out):
@@ -383,6 +392,7 @@ class PagedCache:
         """Cuts every sequence to `budget` slots: new_lens int32 [batch], new_scores like scores, kept int32 [batch, kv_heads, budget].
         new_lens and new_scores may be lens and scores themselves."""
         stream = self._stream(stream)
+        _ints(budget=budget, recent_window=recent_window)
         scores = self._tensors[4]
         for t, like, what in ((new_lens, self._tensors[3], "new_lens"), (new_scores, scores, "new_scores")):
             if like is None:

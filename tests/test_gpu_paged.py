@@ -1,4 +1,6 @@
 """The paged cache (wkv_paged_step, wkv_paged_prefill, wkv_paged_evict) against attention and eviction in 64 bits on the CPU."""
+import ctypes
+
 import pytest
 import torch
 
@@ -508,3 +510,21 @@ def test_the_largest_window(dtype):
     run(p, x=x)
     p = Paged(69, [20, 300], heads=4, kv_heads=2, d=64, dtype=dtype, window=2 ** 31 - 1, sink=2 ** 31 - 1, scores=True)
     run(p)
+
+
+def test_the_workspace_grows_by_steps():
+    """A chunk longer by one token every time does not want a new workspace every time, and all of them stay within a small multiple
+    of what the longest wants."""
+    p = Paged(70, [200], [200], heads=4, kv_heads=2, d=64, scores=True)
+    x = p.device()
+    seen = set()
+    for n in range(1, 201):
+        x["lens"].fill_(n)
+        x["starts"][1] = n
+        x["cache"].prefill(x["q"][:n], x["k_new"][:n], x["v_new"][:n], x["out"][:n], x["starts"], n)
+        seen.add(x["cache"]._at)
+    torch.cuda.synchronize()
+    most = max(wkv._lib.wkv_paged_workspace_bytes(ctypes.byref(x["cache"].c), n, n) for n in range(1, 201))
+    assert len(seen) < 20 and x["cache"]._bytes <= 1.5 * most
+    with pytest.raises(wkv.WkvError, match="32-bit"):
+        x["cache"].evict(2 ** 32 + 9, 1, x["lens"], x["scores"])

@@ -180,3 +180,11 @@ def test_binding_refuses_what_it_cannot_describe():
         with pytest.raises(wkv.WkvError) as e:
             wkv.PagedCache(x["k"], x["v"], x["table"], x["lens"], 4, scores=x["scores"])
         assert e.value.code == wkv.WKV_EINVAL
+
+
+@pytest.mark.parametrize("kw", [dict(heads=2 ** 32 + 4), dict(window=2 ** 32), dict(n_sink=2 ** 31), dict(max_tokens=2 ** 32, max_new=1)])
+def test_binding_refuses_numbers_of_more_than_32_bits(kw):
+    k = torch.zeros(4, 16, 2, 64, dtype=torch.float16)
+    table, lens = torch.zeros(2, 2, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(wkv.WkvError, match="32-bit"):
+        wkv.PagedCache(k, k, table, lens, **{**dict(heads=4), **kw})
