@@ -15,6 +15,11 @@
 // New K and V rows go into their pages on the way: a call reads its own tokens from where they are, so nothing waits for that.
 //
 // Softmax statistics, sums of the weights and of weight . v are fp32.
+//
+// Long steps are bound by memory: 4 x 32768 slots, 32 heads on 8 of 128, fp16: wkv_paged_rows 88.7 us for 537 MB of K and V (6.05 TB/s; 547 MB
+// fetched), the join 4.8.  64 ragged sequences of up to 4096 with logits 131 us for 565 + 19 MB, join and tally 13.3.  Short ones by the chain
+// launch, table, rows, joins: 4096 slots of one sequence 6.3 + 4.0 us, 64 slots in fp32 4.9.  (Waves that keep K and V in registers, one block
+// ahead, and no LDS but for the joins: a first kernel that staged a block at a time took 117 us for the long step, 28 for the one sequence.)
 #include "../../include/wkv.h"
 #include "wkv_internal.h"
 #include "wkv_device.h"
