@@ -528,3 +528,10 @@ def test_the_workspace_grows_by_steps():
     assert len(seen) < 20 and x["cache"]._bytes <= 1.5 * most
     with pytest.raises(wkv.WkvError, match="32-bit"):
         x["cache"].evict(2 ** 32 + 9, 1, x["lens"], x["scores"])
+
+
+def test_many_rows_of_more_than_a_few_parts():
+    """Rows that are joined from five and more parts, as many as fill the chip."""
+    run(Paged(71, [2100], [260], heads=8, kv_heads=1, d=128, dtype="bf16", page=64, scores=True))
+    run(Paged(72, [2100, 2000], [130, 130], heads=8, kv_heads=1, d=64, window=1900, sink=3, missing=[(0, 5)]))
+    run(Paged(73, [700, 5100], heads=1024, kv_heads=1, d=64, page=256, scores=True))
