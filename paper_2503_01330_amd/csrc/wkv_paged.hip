@@ -86,10 +86,22 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
     __shared__ float s_o[WAVES][ROWS][16 * VE + 4];
     __shared__ u32x4_t s_new[WAVES][2 * PIECES];
 
-    int id = blockIdx.x;
-    const int part = id % a.splits; id /= a.splits;
-    const int tile = id % a.tiles;
-    int unit = id / a.tiles;
+    int id = blockIdx.x, tile = 0;
+    if (a.tiles > 1) {
+        // Workgroups are dealt to the chip's eight partitions in turn: the tiles that go over the same keys follow each other on one of them, whose
+        // cache then holds those (64 sequences of 8192 slots, 64 heads on one: 156.6 -> 115.5 us).
+        if ((int)(gridDim.x / a.tiles) % 8 == 0) {
+            const int x = id & 7, y = id >> 3;
+            tile = y % a.tiles;
+            id = y / a.tiles * 8 + x;
+        } else {
+            const int per_unit = a.splits * a.tiles, in = id % per_unit;
+            tile = in / a.splits;
+            id = id / per_unit * a.splits + in % a.splits;
+        }
+    }
+    const int part = id % a.splits;
+    int unit = id / a.splits;
     const WkvPages& c = a.c;
     // Longest sequences first: what is left when the last workgroups have started is short then.
     if (STEP && !EARLY && a.order) {

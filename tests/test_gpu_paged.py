@@ -535,3 +535,11 @@ def test_many_rows_of_more_than_a_few_parts():
     run(Paged(71, [2100], [260], heads=8, kv_heads=1, d=128, dtype="bf16", page=64, scores=True))
     run(Paged(72, [2100, 2000], [130, 130], heads=8, kv_heads=1, d=64, window=1900, sink=3, missing=[(0, 5)]))
     run(Paged(73, [700, 5100], heads=1024, kv_heads=1, d=64, page=256, scores=True))
+
+
+def test_tiles_that_share_keys():
+    """More heads to a K/V head than a tile has rows, in numbers of workgroups that are multiples of the chip's partitions and that are not."""
+    for batch, group, kvh in ((8, 40, 1), (4, 17, 4), (3, 64, 1), (1, 96, 2), (8, 9, 3)):
+        lens = [(37 * i + 41) % 300 for i in range(batch)]
+        run(Paged(74, lens, heads=group * kvh, kv_heads=kvh, d=64, scores=True))
+        run(Paged(75, lens, [min(n, 3) for n in lens], heads=group * kvh, kv_heads=kvh, d=64, scores=True))
