@@ -8,7 +8,7 @@
 //                    S^T = K Q^T leaves in a lane 4 consecutive keys of one row, which is what the second product's operand
 //                    wants (O^T = V^T P^T), so the weights never leave their lane; the values' operand is a transposition of 16-bit
 //                    words within a lane.  The waves' sums are joined through LDS.
-//   wkv_paged_join   the parts of a row joined (join_few: of few parts).
+//   wkv_paged_join   the parts of a row joined (join_few: of few parts, and of many rows).
 //                    Behind the joins in the same launch, the weights of a step are summed for every slot, from the logits that
 //                    wkv_paged_rows left and the parts' sums (tally).
 //   wkv_paged_sums   the weights of a prefill's rows summed for every slot, from the rows' log-sum-exps.
