@@ -5,7 +5,7 @@
 // while one is used.  A wave has 32 rows: S^T = K Q^T on the 32 x 32 x 16 instruction, whose result holds in a lane four consecutive keys
 // of one row at a time, as O^T = V^T P^T takes them for its second operand: weights stay in their lane.  The values' operand, eight keys
 // of one element, is read from LDS transposed.  A softmax with a running reference: the sums are scaled down only where a logit
-// exceeds the reference by more than 8 octaves.
+// exceeds the reference by more than 8 octaves (fp16: 15, with a reference 12 below the logit that sets it).
 //
 // Bound by the matrix and the vector instructions (exponentials, maxima, conversions of the logits), and by the clock, which falls to 1.7 GHz as
 // both fill: 4 x 4096 tokens, 32 heads on 8 of 128, fp16: 622 us, 883 TFLOP/s, the matrix units busy 51 % of the cycles, LDS 26 %, none of these
@@ -77,6 +77,10 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
 {
     using B = Block<D, BK>;
     constexpr int NB = BK / 32, KS = D / 16, DB = D / 32;
+    // The reference may be LAG below a row's largest logit.  In fp16 it is lower by RAISED more, so that weights go up to 2^15, what the format can hold, and
+    // lose bits below SMALL only; with a smaller LAG that is further from the largest.
+    constexpr bool NARROW = __is_same(TT, TF16);
+    constexpr float LAG = NARROW ? 3.f : 8.f, RAISED = NARROW ? 12.f : 0.f, SMALL = 0x1p-14f, MORE = 0x1p29f;
     __shared__ __attribute__((aligned(1024))) char s_kv[4 * B::BYTES];
     const uint32_t s_k0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)s_kv, s_v0 = s_k0 + B::BYTES;
     const uint32_t s_k1 = s_k0 + 2 * B::BYTES, s_v1 = s_k0 + 3 * B::BYTES;
@@ -206,19 +210,84 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
 #pragma unroll
         for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
 
-    auto use = [&](uint32_t kb, uint32_t vb, int pos, const int (&pages)[NG]) __attribute__((always_inline)) {
-        if (pos > p_hi) return;                                            // (the wave's rows are all before it)
-        if constexpr (D > 128) asm("" : "+v"(k_at), "+v"(v_at));          // (addresses made of these are not kept in registers from block to block)
-        f32x16_t s[NB];
+    // S^T of 32 keys
+    auto logits = [&](uint32_t k_at, uint32_t kb) __attribute__((always_inline)) {
+        f32x16_t s = {};
 #pragma unroll
+        for (int i = 0; i < KS; ++i) {
+            const u32x4_t k = *lds_ptr<u32x4_t>((k_at ^ (i << 5)) + kb);
+            s = mfma32<TT>(k, q[i], s);
+        }
+        return s;
+    };
+    // the values' operand of O^T = V^T P^T: 16 keys, elements 32 i and the following
+    auto values = [&](uint32_t v_at, uint32_t vb, int i) __attribute__((always_inline)) {
+        const uint32_t at = (v_at ^ (i << 6)) + vb;
+        const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)lds_ptr<s16x4_t>(at));
+        const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)lds_ptr<s16x4_t>(at + 8 * (D * 2)));
+        const u32x2_t lw = __builtin_bit_cast(u32x2_t, lo), hw = __builtin_bit_cast(u32x2_t, hi);
+        return u32x4_t{lw.x, lw.y, hw.x, hw.y};
+    };
+    auto scale_all = [&](float f) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < DB; ++i)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) o[i][j] *= f;
+    };
+    auto mask = [&](f32x16_t& s, int pos, int page0, int page1) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            const int p = pos + (j >> 2) * 8 + half_q * 4 + (j & 3);
+            const int seen = ((j < 8 ? page0 : page1) >= 0) & (p <= p_row) & ((p > p_row - window) | (p < c.n_sink));
+            s[j] = seen ? s[j] : -INFINITY;
+        }
+    };
+    // What rounding to fp16 took from the block's weights below SMALL, by itself, raised by MORE: half a step of a weight is left of it down to 2^-55 of
+    // a row's largest, and 2^-66 of that one below.  (A key that takes nearly all of a row with a value near 0 leaves the output to such weights.)
+    // Wanted where a logit lies 18 or more below a row's largest.  Looking for that costs 3 to 5 % (4 x 4096 tokens 624 -> 658 us), a prompt that
+    // is full of such logits twice the time (6 times the queries: 1289 us).
+    auto small_weights = [&](uint32_t kb, uint32_t vb, int pos, const int (&pages)[NG], bool full) __attribute__((always_inline)) {
+        const float minus = ref == -INFINITY ? 0.f : -ref;
+#pragma unroll 1
         for (int b = 0; b < NB; ++b) {
-            s[b] = f32x16_t{};
+            uint32_t k_from = k_at, v_from = v_at;        // (addresses and values for this are not kept in registers)
+            asm volatile("" : "+v"(k_from), "+v"(v_from));
+            f32x16_t s = logits(k_from, kb + b * 32 * (D * 2));
+            __builtin_amdgcn_sched_barrier(0);            // (one thing after the other, in few registers)
+            if (!full) mask(s, pos + b * 32, b ? pages[NG - 2] : pages[0], b ? pages[NG - 1] : pages[1]);
+            u32x4_t p[2];
 #pragma unroll
-            for (int i = 0; i < KS; ++i) {
-                const u32x4_t k = *lds_ptr<u32x4_t>((k_at ^ (i << 5)) + kb + b * 32 * (D * 2));
-                s[b] = mfma32<TT>(k, q[i], s[b]);
+            for (int w = 0; w < 8; ++w) {
+                float x[2], y[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[w * 2 + e], a.scale, minus));
+                    x[e] = x[e] < SMALL ? x[e] : 0.f;
+                }
+                unpack2<TT>(pack2<TT>(x[0], x[1]), y[0], y[1]);
+                p[w >> 2][w & 3] = pack2<TT>((x[0] - y[0]) * MORE, (x[1] - y[1]) * MORE);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < DB; ++i) {
+                f32x16_t d = {};
+#pragma unroll
+                for (int j = 0; j < 2; ++j) d = mfma32<TT>(values(v_from, vb + (b * 32 + j * 16) * (D * 2), i), p[j], d);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) o[i][j] = __builtin_fmaf(d[j], 1.f / MORE, o[i][j]);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
+    };
+
+    auto use = [&](uint32_t kb, uint32_t vb, int pos, const int (&pages)[NG]) __attribute__((always_inline)) {
+        if (pos > p_hi) return;                                            // (the wave's rows are all before it)
+        // (addresses made of these are not kept in registers from block to block)
+        if constexpr (D > 128) asm("" : "+v"(k_at), "+v"(v_at));
+        else if constexpr (NARROW) asm("" : "+v"(k_at));
+        f32x16_t s[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) s[b] = logits(k_at, kb + b * 32 * (D * 2));
         const bool full = all_there(pages) && pos + BK - 1 <= p_lo && (pos > p_hi - window || pos + BK <= c.n_sink);
         if (!full) {
 #pragma unroll
@@ -230,6 +299,14 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
                     s[b][j] = seen ? s[b][j] : -INFINITY;
                 }
         }
+        [[maybe_unused]] float low = INFINITY;            // the lowest logit that is seen, of a block that is not full
+        if constexpr (NARROW)
+            if (!full) {
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) low = fminf(low, s[b][j] == -INFINITY ? INFINITY : s[b][j]);
+            }
         float top = s[0][0];
 #pragma unroll
         for (int b = 0; b < NB; ++b)
@@ -240,40 +317,37 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
             lane_pair<32>(top, x0, x1);
             top = fmaxf(x0, x1) * a.scale;
         }
-        if (__any(top > ref + 8.f)) {
-            const float now = fmaxf(ref, top);
+        if (__any(top > ref + (LAG + RAISED))) {
+            const float now = fmaxf(ref, top - RAISED);
             const float f = ref == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref - now);
             ref = now;
             l *= f;
-#pragma unroll
-            for (int i = 0; i < DB; ++i)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) o[i][j] *= f;
+            scale_all(f);
         }
         const float minus = ref == -INFINITY ? 0.f : -ref;
+        [[maybe_unused]] const bool edge = NARROW && !full && __any(__builtin_fmaf(low, a.scale, minus) < -14.f);
+        [[maybe_unused]] float least = MORE;
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
                 s[b][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][j], a.scale, minus));
                 l += s[b][j];
+                if constexpr (NARROW) least = fminf(least, s[b][j]);
             }
 #pragma unroll
             for (int j = 0; j < 2; ++j) {                                  // 16 keys each
-                // weights rounded to the format: an error of the size of the output's own rounding
+                // weights rounded to the format: off by half a step each, and so is the output by half a step of sum w |v|
                 u32x4_t p;
 #pragma unroll
                 for (int w = 0; w < 4; ++w) p[w] = pack2<TT>(s[b][j * 8 + 2 * w], s[b][j * 8 + 2 * w + 1]);
 #pragma unroll
-                for (int i = 0; i < DB; ++i) {
-                    const uint32_t at = (v_at ^ (i << 6)) + vb + (b * 32 + j * 16) * (D * 2);
-                    const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)lds_ptr<s16x4_t>(at));
-                    const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)lds_ptr<s16x4_t>(at + 8 * (D * 2)));
-                    const u32x2_t lw = __builtin_bit_cast(u32x2_t, lo), hw = __builtin_bit_cast(u32x2_t, hi);
-                    const u32x4_t v = {lw.x, lw.y, hw.x, hw.y};
-                    o[i] = mfma32<TT>(v, p, o[i]);
-                }
+                for (int i = 0; i < DB; ++i) o[i] = mfma32<TT>(values(v_at, vb + (b * 32 + j * 16) * (D * 2), i), p, o[i]);
             }
+        }
+        if constexpr (NARROW) {
+            asm volatile("" : "+v"(l));                   // (the weights have been added up: they are not kept for it)
+            if (__builtin_expect(full ? __any(least < SMALL) : edge, 0)) small_weights(kb, vb, pos, pages, full);
         }
     };
 

@@ -153,9 +153,7 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
     const char* kh = c.k + t.h * c.head_bytes;
     const char* vh = c.v + t.h * c.head_bytes;
     const uint32_t k_off = (uint32_t)(col * (int)c.slot_bytes) + g * 16;
-    uint32_t v_off[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v_off[j] = (uint32_t)((g * 4 + j) * (int)c.slot_bytes) + col * (VE * TT::BYTES);
+    const uint32_t v_off = (uint32_t)(g * 4 * (int)c.slot_bytes) + col * (VE * TT::BYTES);
     // A chunk's own tokens, from slot `fresh` on, are read from where they are.  Pages that are not there are loaded as page 0 (it is in the
     // pool) and masked.
     const int fresh = !STEP && a.k_new ? t.pos0 : 0x7FFFFFFF;
@@ -181,7 +179,7 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
 #pragma unroll
             for (int h = 0; h < NH; ++h) {
                 const int p = pos + j / 4 * 16 + g * 4 + j % 4;
-                const char* src = vh + row0(pos + j / 4 * 16, pages[j / 4]) + v_off[j % 4];
+                const char* src = vh + (row0(pos + j / 4 * 16, pages[j / 4]) + j % 4 * c.slot_bytes) + v_off;
                 if (!STEP && p >= fresh && p < t.q.len) src = vf + p * a.v_bytes + col * (VE * TT::BYTES);
                 load_words<VW, STEP>(src + h * (16 * VE * TT::BYTES), x.v[j][h]);
             }
@@ -245,6 +243,13 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
     for (int h = 0; h < NH; ++h)
 #pragma unroll
         for (int e = 0; e < VE; ++e) o[h][e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    constexpr float RAISED = __is_same(TT, TF16) ? 0x1p15f : 1.f;          // what the weights are multiplied by, as operands, and so the sums
+    auto scale_all = [&](float f) {
+#pragma unroll
+        for (int h = 0; h < NH; ++h)
+#pragma unroll
+            for (int e = 0; e < VE; ++e) o[h][e] *= f;
+    };
 
     // one block, and the loads of the next one
     auto use = [&](int pos, const int (&pages)[NT], int next, const int (&next_pages)[NT]) {
@@ -275,6 +280,13 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
                     s[i][j] = seen ? s[i][j] : -INFINITY;
                 }
         }
+        float low = INFINITY;                             // the lowest logit that is seen
+        if constexpr (RAISED != 1.f) {
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) low = fminf(low, full ? s[i][j] : s[i][j] == -INFINITY ? INFINITY : s[i][j]);
+        }
         if constexpr (LOGITS) {
             float* dst = a.logits + ((int64_t)unit * group + row_q) * a.logit_stride + pos + g * 4;
 #pragma unroll
@@ -294,10 +306,7 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
             const float f0 = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - top);
             m = top;
             l *= f0;
-#pragma unroll
-            for (int h = 0; h < NH; ++h)
-#pragma unroll
-                for (int e = 0; e < VE; ++e) o[h][e] *= f0;
+            scale_all(f0);
         }
         const float ref = m == -INFINITY ? 0.f : m;
         float p[NT][4];
@@ -338,7 +347,64 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
                 }
         }
         if constexpr (S::HALF) {
-            // The weights as a sum of two 16-bit numbers: what is left of them is below 2^-16 (bf16) of a weight.  One number
+            // element e of the lane's keys
+            auto values = [&](int h, int e) {
+                u32x4_t vt = {};
+#pragma unroll
+                for (int w = 0; w < VK / 2; ++w)
+                    vt[w] = __builtin_amdgcn_perm(x.v[2 * w + 1][h][e / 2], x.v[2 * w][h][e / 2], (e & 1) ? 0x07060302u : 0x05040100u);
+                return vt;
+            };
+            if constexpr (RAISED != 1.f) {
+                // fp16 has no numbers below 2^-24, so weights are raised by 2^15, up to what it can hold, and those that are still below 2^-9, where the
+                // second number has no bits left, go by themselves, raised by 2^24 more: 2^-16 of a weight down to 2^-48 of a row's largest, and
+                // 2^-64 of that one below.  (A key that takes nearly all of a row with a value near 0 leaves the output to such weights.)
+                constexpr float SMALL = 0x1p-9f, MORE = 0x1p24f;
+#pragma unroll
+                for (int i = 0; i < NT; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) p[i][j] *= RAISED;
+                asm volatile("" : "+v"(l));
+                if (__builtin_expect(__any(__builtin_fmaf(low, a.scale, -ref) < -24.f), 0)) {                // (2^-9, raised)
+                    scale_all(MORE);
+#pragma unroll 1
+                    for (int second = 0; second < 2; ++second) {              // (one number at a time: registers are scarce)
+                        u32x4_t part = {};
+#pragma unroll
+                        for (int w = 0; w < VK / 2; ++w) {
+                            float x0 = p[w >> 1][(w & 1) * 2], x1 = p[w >> 1][(w & 1) * 2 + 1];
+                            x0 = x0 < SMALL ? x0 * MORE : 0.f;
+                            x1 = x1 < SMALL ? x1 * MORE : 0.f;
+                            part[w] = pack2<TT>(x0, x1);
+                            if (second) {
+                                float y0, y1;
+                                unpack2<TT>(part[w], y0, y1);
+                                part[w] = pack2<TT>(x0 - y0, x1 - y1);
+                            }
+                        }
+#pragma unroll
+                        for (int h = 0; h < NH; ++h)
+#pragma unroll
+                            for (int e = 0; e < VE; ++e) {
+                                o[h][e] = mfma<TT>(values(h, e), part, o[h][e]);
+                                __builtin_amdgcn_sched_barrier(0);
+                            }
+                        // (what this makes of the values is not kept in registers)
+#pragma unroll
+                        for (int j = 0; j < VK; ++j)
+#pragma unroll
+                            for (int h = 0; h < NH; ++h)
+#pragma unroll
+                                for (int w = 0; w < VW; ++w) asm volatile("" : "+v"(x.v[j][h][w]));
+                    }
+                    scale_all(1.f / MORE);
+#pragma unroll
+                    for (int i = 0; i < NT; ++i)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) p[i][j] = p[i][j] < SMALL ? 0.f : p[i][j];
+                }
+            }
+            // The weights as a sum of two 16-bit numbers: what is left of them is below 2^-16 of a weight.  One number
             // alone would err as much as the rounding of the output.
             u32x4_t hi = {}, lo = {};
 #pragma unroll
@@ -353,10 +419,7 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
             for (int h = 0; h < NH; ++h)
 #pragma unroll
                 for (int e = 0; e < VE; ++e) {
-                    u32x4_t vt = {};          // element e of the lane's keys
-#pragma unroll
-                    for (int w = 0; w < VK / 2; ++w)
-                        vt[w] = __builtin_amdgcn_perm(x.v[2 * w + 1][h][e / 2], x.v[2 * w][h][e / 2], (e & 1) ? 0x07060302u : 0x05040100u);
+                    const u32x4_t vt = values(h, e);
                     o[h][e] = mfma<TT>(vt, hi, o[h][e]);
                     o[h][e] = mfma<TT>(vt, lo, o[h][e]);
                 }
@@ -421,7 +484,7 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
                 for (int e = g * (D / 4); e < (g + 1) * (D / 4); ++e) dot += load_elem<TT>(qr, e) * load_elem<TT>(kr, e);
                 dot = rows_sum(dot);
                 if (p <= p_row && (p > p_row - window || p < c.n_sink)) {
-                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(dot, a.scale, -ref));
+                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(dot, a.scale, -ref)) * RAISED;
 #pragma unroll
                     for (int h = 0; h < NH; ++h)
 #pragma unroll
@@ -443,7 +506,9 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
     top += JOINED;
     const float share = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
     const bool direct = sp.parts == 1;
-    const int orow = threadIdx.x >> 4, piece = threadIdx.x & 15;           // 16 lanes write a row
+    int tid = threadIdx.x;
+    asm("" : "+v"(tid));                                  // (not kept in registers through the loop above)
+    const int orow = tid >> 4, piece = tid & 15;                           // 16 lanes write a row
     const bool own = r0 + orow < r1;
     float sum = 0.f, otop = s_m[0][orow];
 #pragma unroll
@@ -461,7 +526,7 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int e = 0; e < VE; ++e) s_o[wave][col][(g * 4 + r) * VE + e] = o[h][e][r] * share;
+            for (int e = 0; e < VE; ++e) s_o[wave][col][(g * 4 + r) * VE + e] = o[h][e][r] * (share * (1.f / RAISED));
         __syncthreads();
         float x[VE];
 #pragma unroll
