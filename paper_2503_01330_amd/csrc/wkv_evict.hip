@@ -237,15 +237,16 @@ void wkv_evict_move_kernel(const WkvPages c, int list_stride, int pieces, int ei
 hipError_t wkv_launch_paged_evict(const WkvPages& c, int row_bytes, int budget, int recent, int32_t* new_lens, float* new_scores,
                                   int32_t* kept, int32_t* plan, int32_t* list, hipStream_t stream)
 {
-    constexpr int PIECE = 64;         // of 128 bytes, few units leave half the chip idle (4 x 32768 slots of 8 heads to 2048: 18.5 us, 13.5 of 64)
+    // (pieces of 128 bytes leave half the chip idle where there are few units: 4 x 32768 slots of 8 heads to 2048: 18.5 us, 13.5 of 64)
+    constexpr int PIECE = WKV_EVICT_PIECE;
     const int units = c.batch * c.kv_heads, pieces = row_bytes / PIECE, list_stride = std::min(budget, c.max_slots);
-    const int per_unit = 2 * pieces + 1, eights = (units + 7) / 8 * 8;
+    const int eights = (units + 7) / 8 * 8;
     // (sequences of up to 4096 slots: 8 us with 4 scores a thread, 17 with 32)
     if (c.max_slots <= 4 * THREADS) hipLaunchKernelGGL((wkv_evict_select_kernel<4>), dim3(units), dim3(THREADS), 0, stream, c, budget, list_stride, recent, kept, plan, list);
     else hipLaunchKernelGGL((wkv_evict_select_kernel<32>), dim3(units), dim3(THREADS), 0, stream, c, budget, list_stride, recent, kept, plan, list);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((wkv_evict_move_kernel<PIECE>), dim3(eights * per_unit), dim3(THREADS), 0, stream, c, list_stride, pieces, eights, budget, kept,
+    hipLaunchKernelGGL((wkv_evict_move_kernel<PIECE>), dim3((unsigned)wkv_evict_groups(units, row_bytes)), dim3(THREADS), 0, stream, c, list_stride, pieces, eights, budget, kept,
                        plan, list, new_lens, new_scores);
     return hipGetLastError();
 }

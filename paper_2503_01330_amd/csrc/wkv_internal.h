@@ -156,6 +156,11 @@ int64_t wkv_paged_most_keys(const WkvPages& c, int64_t new_tokens);
 // of which there are most_keys at most: fills many, tiles, splits, tile_rows, block, least and order.
 void wkv_paged_shape(WkvPagedCall& a, int64_t units, int64_t rows, int64_t most_keys, int dtype, int head_dim, bool step);
 
+// Workgroups of 1024 threads that move what is left: of a unit, those for each piece of K's and V's rows and one for the sums; and of all units,
+// which run in eights.
+constexpr int WKV_EVICT_PIECE = 64;
+inline int64_t wkv_evict_per_unit(int row_bytes) { return 2 * (row_bytes / WKV_EVICT_PIECE) + 1; }
+inline int64_t wkv_evict_groups(int64_t units, int row_bytes) { return (units + 7) / 8 * 8 * wkv_evict_per_unit(row_bytes); }
 // plan: [batch][2] lengths before and after; list: [unit][budget] slots that are left, ascending
 hipError_t wkv_launch_paged_evict(const WkvPages& c, int row_bytes, int budget, int recent, int32_t* new_lens, float* new_scores,
                                   int32_t* kept, int32_t* plan, int32_t* list, hipStream_t stream);

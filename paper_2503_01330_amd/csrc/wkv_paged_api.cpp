@@ -215,7 +215,7 @@ int wkv_paged_evict(const wkv_paged* c, int budget, int recent_window, int32_t* 
     if (budget < 1 || recent_window < 1 || (int64_t)c->n_sink + recent_window > budget)
         return fail(WKV_EINVAL, "1 <= recent_window and n_sink + recent_window <= budget are wanted: %d, %d, %d", recent_window, c->n_sink, budget);
     const WkvPages p = pages_of(*c);
-    if ((int64_t)c->batch * c->kv_heads * (c->head_dim * elem_bytes(c->dtype) / 32 + 1) >= 1 << 22)
+    if (wkv_evict_groups((int64_t)c->batch * c->kv_heads, c->head_dim * elem_bytes(c->dtype)) >= 1 << 22)
         return fail(WKV_ESIZE, "%d units: a launch holds fewer than 2^32 threads", c->batch * c->kv_heads);
     // (a budget that no sequence can exceed leaves all of them as they are)
     rc = check_work(workspace, workspace_bytes, evict_bytes(*c, std::min(budget, p.max_slots)));
