@@ -55,7 +55,7 @@ void wkv_evict_select_kernel(const WkvPages c, int budget, int list_stride, int 
     if (h == 0 && tid == 0) { plan[2 * b] = len; plan[2 * b + 1] = whole ? len : budget; }
     if (whole) {
         if (out)
-            for (int i = tid; i < budget; i += THREADS) out[i] = !missing && i < len ? i : -1;
+            for (unsigned i = tid; i < (unsigned)budget; i += THREADS) out[i] = !missing && (int)i < len ? (int)i : -1;      // (a budget may be 2^31 - 1)
         return;
     }
 
