@@ -617,6 +617,12 @@ __device__ __forceinline__ void tally(const WkvPagedCall& a, int block, int per_
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         if (first + i * THREADS + (int)threadIdx.x >= keys) continue;
+        if (w[i] != w[i]) {
+            // some row has no finite weights, which gives it none on what it does not see either: a missing page, or what lies beside the window in its blocks
+            const int page = a.c.table[t.b * a.c.table_stride + (at[i] >> a.c.page_shift)];
+            const bool seen = (unsigned)page < (unsigned)a.c.n_pages && (a.c.window <= 0 || at[i] > t.pos0 - a.c.window || at[i] < a.c.n_sink);
+            w[i] = seen ? w[i] : 0.f;
+        }
         if (at[i] == t.pos0 && a.k_new) sc[at[i]] = w[i];
         else sc[at[i]] += w[i];
     }
