@@ -301,6 +301,10 @@ class PagedCache:
     scores: float32 [batch, kv_heads, n], n within the last page, or None
     The tensors are kept alive; what they hold is read when a call runs.  Calls on one object must not overlap in time
     (the workspace is one); another object over the same tensors has its own.
+
+    A call runs on the current stream, or on `stream` (its address), whichever that is: the workspace's memory is given back when the streams
+    that it was used on have got past it.  A stream that is no torch stream has to exist as long as the object, and the object as long as a
+    HIP graph that has recorded its calls.
     """
 
     def __init__(self, k, v, table, lens, heads, window=0, n_sink=0, scores=None, max_tokens=0, max_new=0):
@@ -332,15 +336,31 @@ class PagedCache:
         self._work = None
         self._reserve(max_tokens, max_new)
 
-    def _reserve(self, n_tokens, max_new):
+    def _reserve(self, n_tokens, max_new, stream=None):
         need = _lib.wkv_paged_workspace_bytes(C.byref(self.c), n_tokens, max_new)
         if need == 0:
             _refuse("no workspace for these sizes: " + wkv_last_error())
         have = 0 if self._work is None else self._work.numel()
         if have < need:
-            self._kept.append(self._work)               # (work on another stream may still be using it, or a recorded graph)
-            self._work = torch.empty(max(need, have + have // 2), dtype=torch.uint8, device=self.device)        # (all of those: twice this one)
+            self._grow(max(need, have + have // 2), stream)          # (all that are kept: twice this one)
         self._at, self._bytes = self._work.data_ptr(), self._work.numel()
+
+    def _grow(self, size, stream):
+        home = torch.cuda.current_stream(self.device)
+        for s in (home, *([] if stream is None else [torch.cuda.ExternalStream(stream, device=self.device)])):
+            with torch.cuda.stream(s):
+                if torch.cuda.is_current_stream_capturing():
+                    _refuse("no workspace is taken while a graph is recorded: make a call of these sizes before, or an object with these max_tokens and max_new")
+        work = torch.empty(size, dtype=torch.uint8, device=self.device)
+        # What had the memory before may still run on the stream that it is taken on, which other streams do not wait for.
+        home.synchronize()
+        self._kept.append(self._work)                       # (work on another stream may still be using it, or a recorded graph)
+        self._work, self._streams = work, {home.cuda_stream}
+
+    def _used_on(self, stream):
+        """The workspace's memory waits for this stream too before it is anyone else's."""
+        self._work.record_stream(torch.cuda.ExternalStream(stream, device=self.device))
+        self._streams.add(stream)
 
     def _fill(self, n, q, k, v, out):
         """The rows of a call, n tokens."""
@@ -369,6 +389,8 @@ class PagedCache:
         (appended already).  Any strides that are multiples of 16 bytes.  lens counts the new tokens."""
         stream = self._stream(stream)
         self._fill(self.batch, q, k_new, v_new, out)
+        if stream not in self._streams:
+            self._used_on(stream)
         rc = _paged_step(self._ref, self._rows_ref, self._at, self._bytes, stream)
         if rc:
             _check(rc)
@@ -385,7 +407,9 @@ class PagedCache:
             _refuse("starts: int32 [batch + 1] on the cache's GPU")
         if not 1 <= max_new <= n:
             _refuse(f"1 <= max_new <= n_tokens is wanted: {max_new}, {n}")
-        self._reserve(n, max_new)
+        self._reserve(n, max_new, stream)
+        if stream not in self._streams:
+            self._used_on(stream)
         _check(_lib.wkv_paged_prefill(self._ref, self._rows_ref, starts.data_ptr(), n, max_new, self._at, self._bytes, stream))
 
     def evict(self, budget, recent_window, new_lens, new_scores, kept=None, stream=None):
@@ -402,5 +426,7 @@ class PagedCache:
         if kept is not None and (kept.dtype != torch.int32 or tuple(kept.shape) != (self.batch, self.kv_heads, budget)
                                  or not kept.is_contiguous() or kept.device != self.device):
             _refuse("kept: int32 [batch, kv_heads, budget]")
+        if stream not in self._streams:
+            self._used_on(stream)
         _check(_lib.wkv_paged_evict(self._ref, budget, recent_window, new_lens.data_ptr(), new_scores.data_ptr(),
                                     kept.data_ptr() if kept is not None else None, self._at, self._bytes, stream))
