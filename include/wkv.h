@@ -318,7 +318,7 @@ typedef struct wkv_paged_rows {
 } wkv_paged_rows;
 
 /* Bytes of DEVICE workspace (16-byte aligned) that wkv_paged_step, wkv_paged_evict and a wkv_paged_prefill with these
- * n_tokens and max_new (0, 0: none) want for this cache; 0 if the description is invalid.  Fewer tokens with the same
+ * n_tokens and max_new (0, 0: none) want for this cache; 0 if the description is invalid or such a prefill would be refused for its size.  Fewer tokens with the same
  * max_new want no more; another max_new, smaller or larger, may.
  * The contents do not matter before a call, nor after it.  Calls that share a workspace must not overlap in time,
  * recorded ones (HIP graphs) included.  Host-only arithmetic; pointers are not looked at, but for scores being NULL or not. */
@@ -338,7 +338,8 @@ int wkv_paged_step(const wkv_paged* c, const wkv_paged_rows* rows, void* workspa
  * tokens of sequence b, in slots lens[b]-n .. lens[b]-1.  Appends k and v, attends, and with scores adds the weights, all queries' and heads' of the group together (appended slots' sums start with this).
  *   starts  : DEVICE int32 [batch+1], not decreasing; rows behind starts[batch] are left as they are
  *   n_tokens: tokens that the rows have; max_new: at least the longest chunk (longer ones are cut to it), at
- *             most n_tokens and 2^24; n_tokens*heads is at most 2^30.  A chunk longer than its sequence's lens[b]: its first rows have no slot; they see nothing.
+ *             most n_tokens and 2^24; n_tokens*heads is at most 2^30 (fp32: about 2^26 where chunks differ in length), batch*kv_heads
+ *             below about 2^23.  A chunk longer than its sequence's lens[b]: its first rows have no slot; they see nothing.
  * Asynchronous as wkv_paged_step.  How the work is shared out depends on the sizes (not on lens), and so do last bits;
  * the same call gives the same bits every time.
  */

@@ -87,9 +87,12 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
 
     // Workgroups are dealt to the chip's eight partitions in turn: with spread, all of a unit's go to one of them, whose cache then
     // holds the unit's K and V.  Tiles far into the sequence, which have the most keys, come first.
-    int id = blockIdx.x, unit;
+    int id = blockIdx.x, unit, tile, part = 0;
     const int per_unit = tiles * a.splits;
-    if (spread) {
+    if (a.slots > 0) {
+        // (a K/V head's on one partition where there are 8 of them, or 16, ...)
+        if (!packed_tile(a, id % a.c.kv_heads, a.slots - 1 - id / a.c.kv_heads, unit, tile)) return;
+    } else if (spread) {
         const int x = id & 7;
         id >>= 3;
         unit = id / per_unit * 8 + x;
@@ -98,7 +101,10 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
         unit = id / per_unit;
         id = id % per_unit;
     }
-    const int part = id % a.splits, tile = tiles - 1 - id / a.splits;
+    if (a.slots == 0) {
+        part = id % a.splits;
+        tile = tiles - 1 - id / a.splits;
+    }
     Tile t;
     if (!unit_of<false>(a, unit, tile * TILE_ROWS, t)) return;
     const WkvPages& c = a.c;
@@ -683,7 +689,7 @@ hipError_t wkv_launch_paged_flash(const WkvPagedCall& a, int dtype, int head_dim
     auto go = [&](auto t, auto d, auto bk) {
         using TT = decltype(t);
         constexpr int D = decltype(d)::value, BK = decltype(bk)::value;
-        hipLaunchKernelGGL((wkv_paged_flash_kernel<TT, D, BK>), dim3((unsigned)((int64_t)units * tiles * a.splits)), dim3(THREADS), 0, stream, a, tiles, spread);
+        hipLaunchKernelGGL((wkv_paged_flash_kernel<TT, D, BK>), dim3((unsigned)wkv_paged_groups(a)), dim3(THREADS), 0, stream, a, tiles, spread);
         return hipGetLastError();
     };
     auto wide = [&](auto t) {

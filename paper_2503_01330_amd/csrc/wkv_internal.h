@@ -135,6 +135,7 @@ struct WkvPagedCall {
     int tiles, splits;               // row tiles of 16 per unit (sequence, K/V head); parts that a tile's keys are cut into at most
     bool many;                       // the kernel for many rows (wkv_flash.hip) and not the one for few
     int tile_rows, block, least;     // that kernel's rows a tile, keys a block, blocks a part at least
+    int slots;                       // not 0: a launch for chunks of different lengths, with room for this many tiles of a K/V head (packed_tile)
     int order;                       // a step: workgroups take the longest sequences first
     float* part;                     // [unit][tile][split][16][head_dim] sums of weight . v, when splits > 1
     float* ml;                       // [unit][tile][split][2][16] reference (log2) and sum of the weights
@@ -145,6 +146,13 @@ struct WkvPagedCall {
     float* lse;                      // [n_tokens][heads] log2 of the sum of exp(logit), of a prefill whose weights are summed, or null
 };
 
+// Workgroups of the call's first launch.
+inline int64_t wkv_paged_groups(const WkvPagedCall& a)
+{
+    if (a.slots) return (int64_t)a.slots * a.c.kv_heads;
+    const int64_t rows = (int64_t)a.max_new * a.c.group;
+    return (int64_t)a.c.batch * a.c.kv_heads * ((rows + a.tile_rows - 1) / a.tile_rows) * a.splits;
+}
 hipError_t wkv_launch_paged_attend(const WkvPagedCall& a, int dtype, int head_dim, hipStream_t stream);
 hipError_t wkv_launch_paged_sums(const WkvPagedCall& a, int dtype, int head_dim, hipStream_t stream);
 int wkv_paged_row_parts(int64_t units, int64_t slots, int64_t rows);
@@ -153,7 +161,7 @@ hipError_t wkv_launch_paged_flash(const WkvPagedCall& a, int dtype, int head_dim
 // Most keys that a query sees, or the queries of new_tokens tokens next to each other.
 int64_t wkv_paged_most_keys(const WkvPages& c, int64_t new_tokens);
 // Which kernel a call of `rows` rows a unit at most takes (a step: always the one for few), and into how many parts it cuts a tile's keys,
-// of which there are most_keys at most: fills many, tiles, splits, tile_rows, block, least and order.
+// of which there are most_keys at most: fills many, tiles, splits, tile_rows, block, least, slots and order.  (a.c, a.n_tokens and a.max_new are there.)
 void wkv_paged_shape(WkvPagedCall& a, int64_t units, int64_t rows, int64_t most_keys, int dtype, int head_dim, bool step);
 
 // Workgroups of 1024 threads that move what is left: of a unit, those for each piece of K's and V's rows and one for the sums; and of all units,

@@ -86,8 +86,11 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
     __shared__ float s_o[WAVES][ROWS][16 * VE + 4];
     __shared__ u32x4_t s_new[WAVES][2 * PIECES];
 
-    int id = blockIdx.x, tile = 0;
-    if (a.tiles > 1) {
+    int id = blockIdx.x, tile = 0, unit = 0;
+    const bool packed = !STEP && a.slots > 0;
+    if (packed) {
+        if (!packed_tile(a, id % a.c.kv_heads, id / a.c.kv_heads, unit, tile)) return;
+    } else if (a.tiles > 1) {
         // Workgroups are dealt to the chip's eight partitions in turn: the tiles that go over the same keys follow each other on one of them, whose
         // cache then holds those (64 sequences of 8192 slots, 64 heads on one: 156.6 -> 115.5 us).
         if ((int)(gridDim.x / a.tiles) % 8 == 0) {
@@ -100,8 +103,8 @@ void wkv_paged_rows_kernel(const WkvPagedCall a)
             id = id / per_unit * a.splits + in % a.splits;
         }
     }
-    const int part = id % a.splits;
-    int unit = id / a.splits;
+    const int part = packed ? 0 : id % a.splits;
+    if (!packed) unit = id / a.splits;
     const WkvPages& c = a.c;
     // Longest sequences first: what is left when the last workgroups have started is short then.
     if (STEP && !EARLY && a.order) {
@@ -842,6 +845,16 @@ void wkv_paged_shape(WkvPagedCall& a, int64_t units, int64_t rows, int64_t most,
     const int64_t groups = units * ((rows + a.tile_rows - 1) / a.tile_rows);
     auto over = [&](int64_t n) { return (n + groups - 1) / groups; };
     auto parts = [&](int64_t want, int64_t least) { return (int)std::max<int64_t>(1, std::min<int64_t>({want, (most + least - 1) / least, 64})); };
+    // Chunks of different lengths: room for the tiles that n_tokens can have, where as many as the longest chunk has for every sequence are several times
+    // that.  us with a workgroup for each of those | packed: 64 chunks of 128 tokens and one of 512 (3 times) 136 | 138, of 128 and 1024 (6) 148 | 155,
+    // 200 of 64 and 1024 (10) 109 | 100, 64 of 64 and 2048 (16) 165 | 139, 256 of 4 and 8192 (121) 1104 | 670; the other kernel, fp32, 128 of 64 and 512
+    // (3) 104 | 84, of 16 and 1024 (7) 132 | 56.
+    a.slots = 0;
+    auto pack = [&] {
+        if (step || a.splits > 1) return;
+        const int64_t slots = (int64_t)a.n_tokens * a.c.group / a.tile_rows + a.c.batch;
+        if (groups > (a.many ? 8 : 2) * slots * a.c.kv_heads) a.slots = (int)slots;
+    };
     if (a.many) {
         // Parts of 384 keys at least, as many as three workgroups a compute unit want; two for a prompt, whose tiles are of different lengths anyway.
         // us with 256 | 512 | 768 workgroups wanted: 3 x 333 tokens on 6001 190 | 159 | 171, of ragged lengths 185 | 120 | 99, 2 x 500 on 16000 489 | 359 | 336,
@@ -849,6 +862,7 @@ void wkv_paged_shape(WkvPagedCall& a, int64_t units, int64_t rows, int64_t most,
         a.splits = parts(over((int64_t)a.max_new * 2 > a.c.max_slots ? 512 : 768), 384);
         a.block = head_dim == 64 || (head_dim == 128 && groups * a.splits <= 512) ? 64 : 32;
         a.least = 384 / a.block;
+        pack();
         return;
     }
     a.block = dtype == WKV_FP32 || head_dim > 128 ? 16 : 32;
@@ -860,6 +874,7 @@ void wkv_paged_shape(WkvPagedCall& a, int64_t units, int64_t rows, int64_t most,
     a.splits = parts(std::max(over(256), std::min(over(768), most / 1024)), (int64_t)a.block * a.least);
     // More workgroups than run at once: the longest sequences first (64 ragged sequences, 1024 workgroups: 157 -> 148 us).
     a.order = step && a.c.batch > 1 && groups * a.splits > 768;
+    pack();
 }
 
 hipError_t wkv_launch_paged_attend(const WkvPagedCall& a, int dtype, int head_dim, hipStream_t stream)
@@ -869,7 +884,7 @@ hipError_t wkv_launch_paged_attend(const WkvPagedCall& a, int dtype, int head_di
         using TT = decltype(t);
         constexpr int D = decltype(d)::value;
         const WkvPages& c = a.c;
-        const dim3 grid((unsigned)(units * a.tiles * a.splits)), block(THREADS);
+        const dim3 grid((unsigned)wkv_paged_groups(a)), block(THREADS);
         hipError_t e = hipSuccess;
         // (a workgroup's start is early where all of them start at once)
         const bool early = c.window == 0 && !a.order;

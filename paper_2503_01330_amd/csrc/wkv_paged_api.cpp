@@ -100,6 +100,7 @@ Layout layout(const wkv_paged& p, bool scores, int n_tokens, int max_new, bool s
     Layout l;
     const int64_t rows = (int64_t)max_new * c.group;
     l.shape.c = c;
+    l.shape.n_tokens = n_tokens;
     l.shape.max_new = max_new;
     wkv_paged_shape(l.shape, units, rows, wkv_paged_most_keys(c, std::min(max_new, 128 / c.group + 2)), p.dtype, p.head_dim, step);
     auto take = [&](size_t bytes) { const size_t at = l.total; l.total += (bytes + 255) / 256 * 256; return at; };
@@ -118,6 +119,16 @@ Layout layout(const wkv_paged& p, bool scores, int n_tokens, int max_new, bool s
 size_t evict_bytes(const wkv_paged& p, int budget)
 {
     return ((size_t)p.batch * 8 + 255) / 256 * 256 + (size_t)p.batch * p.kv_heads * budget * sizeof(int32_t);
+}
+
+// A launch of 2^32 threads and more is not refused by the runtime: the count wraps.
+int check_launch(const WkvPagedCall& a)
+{
+    // (room for tiles of chunks of different lengths: half of what a launch holds)
+    const int64_t groups = wkv_paged_groups(a);
+    if (groups >= (a.slots ? 1 << 23 : 1 << 24))
+        return fail(WKV_ESIZE, "%lld workgroups of 256 threads: a launch holds fewer than 2^32 threads", (long long)groups);
+    return WKV_OK;
 }
 
 int check_work(const void* workspace, size_t have, size_t need)
@@ -149,6 +160,8 @@ int attend(const wkv_paged* p, const wkv_paged_rows* r, const int32_t* starts, i
     rc = check_chunk(*p, n_tokens, max_new);
     if (rc != WKV_OK) return rc;
     const Layout l = layout(*p, p->scores != nullptr, n_tokens, max_new, step);
+    rc = check_launch(l.shape);
+    if (rc != WKV_OK) return rc;
     rc = check_work(workspace, workspace_bytes, l.total);
     if (rc != WKV_OK) return rc;
     WkvPagedCall a = l.shape;
@@ -164,10 +177,7 @@ int attend(const wkv_paged* p, const wkv_paged_rows* r, const int32_t* starts, i
     if (p->scores && step) a.logits = (float*)(w + l.logits);
     if (p->scores && !step) a.lse = (float*)(w + l.lse);
     if (a.row_parts > 1) a.colsums = (float*)(w + l.colsums);
-    // a launch of 2^32 threads and more is not refused by the runtime: the count wraps
     const int64_t units = (int64_t)p->batch * p->kv_heads;
-    if (units * a.tiles * a.splits >= 1 << 24)
-        return fail(WKV_ESIZE, "%lld row tiles in %d parts: a launch holds fewer than 2^32 threads", (long long)(units * a.tiles), a.splits);
     if (a.logits && units * ((a.c.max_slots + 1023) / 1024) >= (1 << 23) - (1 << 16))
         return fail(WKV_ESIZE, "%lld units of %d slots: a launch holds fewer than 2^32 threads", (long long)units, a.c.max_slots);
     hipError_t e = wkv_launch_paged_attend(a, p->dtype, p->head_dim, stream);
@@ -184,7 +194,11 @@ size_t wkv_paged_workspace_bytes(const wkv_paged* c, int n_tokens, int max_new)
     if (!c || check_shape(*c) != WKV_OK || n_tokens < 0 || max_new < 0 || max_new > n_tokens || check_chunk(*c, n_tokens, max_new) != WKV_OK) return 0;
     const bool scores = c->scores != nullptr;
     size_t need = std::max(layout(*c, scores, c->batch, 1, true).total, (size_t)256);
-    if (max_new > 0) need = std::max(need, layout(*c, scores, n_tokens, max_new, false).total);
+    if (max_new > 0) {
+        const Layout l = layout(*c, scores, n_tokens, max_new, false);
+        if (check_launch(l.shape) != WKV_OK) return 0;
+        need = std::max(need, l.total);
+    }
     if (scores) need = std::max(need, evict_bytes(*c, pages_of(*c).max_slots));
     return need;
 }

@@ -117,6 +117,27 @@ template <bool STEP> __device__ __forceinline__ bool unit_of(const WkvPagedCall&
     return row < t.rows;
 }
 
+// Chunks of different lengths: K/V head h's tile x of all that there is room for, a tile having a.tile_rows rows.  Sequence b's tiles are those from
+// base(b) = starts[b] * group / rows + b on, as many as its rows fill; base(b + 1) is behind the last of them, for the quotient of a sum is at
+// most 1 more than the quotients' sum.  The wave looks for b among 64 at a time.  (Of starts that decrease some sequence is found, or none.)
+__device__ __forceinline__ bool packed_tile(const WkvPagedCall& a, int h, int x, int& unit, int& tile)
+{
+    auto base = [&](int b) { return min(max(a.starts[b], 0), a.n_tokens) * a.c.group / a.tile_rows + b; };
+    const int lane = threadIdx.x & 63;
+    int b = 0, n = a.c.batch;                             // it is one of the n from b on
+    while (n > 1) {
+        const int step = (n + 63) / 64;
+        const int before = __popcll(__ballot(lane * step < n && base(b + min(lane * step, n - 1)) <= x));
+        const int k = max(before - 1, 0) * step;
+        b += k;
+        n = min(step, n - k);
+    }
+    b = __builtin_amdgcn_readfirstlane(b);
+    tile = x - base(b);
+    unit = b * a.c.kv_heads + h;
+    return (unsigned)tile < (unsigned)((a.max_new * a.c.group + a.tile_rows - 1) / a.tile_rows);
+}
+
 // Tokens [first, last) of the unit's sequence into their pages, where those are there.
 template <int ROW_BYTES, int THREADS>
 __device__ __forceinline__ void append_rows(const WkvPagedCall& a, const Tile& t, int first, int last)
