@@ -242,11 +242,9 @@ hipError_t wkv_launch_paged_evict(const WkvPages& c, int row_bytes, int budget, 
     const int units = c.batch * c.kv_heads, pieces = row_bytes / PIECE, list_stride = std::min(budget, c.max_slots);
     const int eights = (units + 7) / 8 * 8;
     // (sequences of up to 4096 slots: 8 us with 4 scores a thread, 17 with 32)
-    if (c.max_slots <= 4 * THREADS) hipLaunchKernelGGL((wkv_evict_select_kernel<4>), dim3(units), dim3(THREADS), 0, stream, c, budget, list_stride, recent, kept, plan, list);
-    else hipLaunchKernelGGL((wkv_evict_select_kernel<32>), dim3(units), dim3(THREADS), 0, stream, c, budget, list_stride, recent, kept, plan, list);
-    hipError_t e = hipGetLastError();
+    const hipError_t e = wkv_launch(c.max_slots <= 4 * THREADS ? &wkv_evict_select_kernel<4> : &wkv_evict_select_kernel<32>, units, THREADS, stream, c, budget,
+                                    list_stride, recent, kept, plan, list);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((wkv_evict_move_kernel<PIECE>), dim3((unsigned)wkv_evict_groups(units, row_bytes)), dim3(THREADS), 0, stream, c, list_stride, pieces, eights, budget, kept,
-                       plan, list, new_lens, new_scores);
-    return hipGetLastError();
+    return wkv_launch(&wkv_evict_move_kernel<PIECE>, (unsigned)wkv_evict_groups(units, row_bytes), THREADS, stream, c, list_stride, pieces, eights, budget, kept,
+                      (const int32_t*)plan, (const int32_t*)list, new_lens, new_scores);
 }

@@ -666,14 +666,13 @@ hipError_t wkv_launch_paged_colsum(const WkvPagedCall& a, int dtype, int head_di
         constexpr int D = decltype(d)::value;
         for (int64_t b = 0; b < all;) {                 // in pieces below 2^32 threads
             const int64_t n = std::min<int64_t>(all - b, most);
-            hipLaunchKernelGGL((wkv_paged_colsum_kernel<TT, D>), dim3((unsigned)(n * fast * a.row_parts)), dim3(THREADS), 0, stream, a, by_unit, fast, b);
+            const hipError_t e = wkv_launch(&wkv_paged_colsum_kernel<TT, D>, (unsigned)(n * fast * a.row_parts), THREADS, stream, a, by_unit, fast, b);
+            if (e != hipSuccess) return e;
             b += n;
         }
-        if (a.row_parts > 1) {
-            const int per_unit = (a.c.max_slots + THREADS - 1) / THREADS;
-            hipLaunchKernelGGL(wkv_paged_colsum_join_kernel, dim3((unsigned)(units * per_unit)), dim3(THREADS), 0, stream, a, per_unit);
-        }
-        return hipGetLastError();
+        if (a.row_parts == 1) return hipSuccess;
+        const int per_unit = (a.c.max_slots + THREADS - 1) / THREADS;
+        return wkv_launch(&wkv_paged_colsum_join_kernel, (unsigned)(units * per_unit), THREADS, stream, a, per_unit);
     };
     auto size = [&](auto t) {
         return head_dim == 64 ? go(t, std::integral_constant<int, 64>{}) : head_dim == 128 ? go(t, std::integral_constant<int, 128>{})
@@ -689,8 +688,7 @@ hipError_t wkv_launch_paged_flash(const WkvPagedCall& a, int dtype, int head_dim
     auto go = [&](auto t, auto d, auto bk) {
         using TT = decltype(t);
         constexpr int D = decltype(d)::value, BK = decltype(bk)::value;
-        hipLaunchKernelGGL((wkv_paged_flash_kernel<TT, D, BK>), dim3((unsigned)wkv_paged_groups(a)), dim3(THREADS), 0, stream, a, tiles, spread);
-        return hipGetLastError();
+        return wkv_launch(&wkv_paged_flash_kernel<TT, D, BK>, (unsigned)wkv_paged_groups(a), THREADS, stream, a, tiles, spread);
     };
     auto wide = [&](auto t) {
         constexpr std::integral_constant<int, 32> few{};

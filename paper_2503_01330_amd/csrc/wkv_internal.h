@@ -6,6 +6,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 // Device-resident cache of one handle: m = budget physical slots per unit.
 //
 // While a step runs, the cache logically has m+1 entries (Algorithm 1 computes
@@ -145,6 +147,15 @@ struct WkvPagedCall {
     float* colsums;                  // [row part][unit][logit_stride] their sums, when row_parts > 1
     float* lse;                      // [n_tokens][heads] log2 of the sum of exp(logit), of a prefill whose weights are summed, or null
 };
+
+// One launch, and its own error: hipGetLastError would also give one that an earlier call of the program has left behind.
+template <class... P, class... A>
+hipError_t wkv_launch(void (*kernel)(P...), unsigned groups, unsigned threads, hipStream_t stream, const A&... args)
+{
+    static_assert((std::is_same<std::remove_const_t<P>, A>::value && ...), "arguments are passed as they are");
+    void* list[] = { (void*)&args... };
+    return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3(groups), dim3(threads), list, 0, stream);
+}
 
 // Workgroups of the call's first launch.
 inline int64_t wkv_paged_groups(const WkvPagedCall& a)

@@ -884,17 +884,16 @@ hipError_t wkv_launch_paged_attend(const WkvPagedCall& a, int dtype, int head_di
         using TT = decltype(t);
         constexpr int D = decltype(d)::value;
         const WkvPages& c = a.c;
-        const dim3 grid((unsigned)wkv_paged_groups(a)), block(THREADS);
-        hipError_t e = hipSuccess;
+        const unsigned grid = (unsigned)wkv_paged_groups(a);
+        hipError_t e;
         // (a workgroup's start is early where all of them start at once)
         const bool early = c.window == 0 && !a.order;
         if (a.many) e = wkv_launch_paged_flash(a, dtype, head_dim, stream);
-        else if (a.starts) hipLaunchKernelGGL((wkv_paged_rows_kernel<TT, D, false, false, false>), grid, block, 0, stream, a);
-        else if (early && !a.logits) hipLaunchKernelGGL((wkv_paged_rows_kernel<TT, D, true, true, false>), grid, block, 0, stream, a);
-        else if (early) hipLaunchKernelGGL((wkv_paged_rows_kernel<TT, D, true, true, true>), grid, block, 0, stream, a);
-        else if (!a.logits) hipLaunchKernelGGL((wkv_paged_rows_kernel<TT, D, true, false, false>), grid, block, 0, stream, a);
-        else hipLaunchKernelGGL((wkv_paged_rows_kernel<TT, D, true, false, true>), grid, block, 0, stream, a);
-        if (e == hipSuccess) e = hipGetLastError();
+        else if (a.starts) e = wkv_launch(&wkv_paged_rows_kernel<TT, D, false, false, false>, grid, THREADS, stream, a);
+        else if (early && !a.logits) e = wkv_launch(&wkv_paged_rows_kernel<TT, D, true, true, false>, grid, THREADS, stream, a);
+        else if (early) e = wkv_launch(&wkv_paged_rows_kernel<TT, D, true, true, true>, grid, THREADS, stream, a);
+        else if (!a.logits) e = wkv_launch(&wkv_paged_rows_kernel<TT, D, true, false, false>, grid, THREADS, stream, a);
+        else e = wkv_launch(&wkv_paged_rows_kernel<TT, D, true, false, true>, grid, THREADS, stream, a);
         if (e == hipSuccess && (a.splits > 1 || a.logits)) {
             const int per_tile = (int)std::min<int64_t>(ROWS, (int64_t)a.max_new * a.c.group);
             const int rows = a.splits > 1 ? (int)(units * a.tiles * per_tile) : 0;
@@ -903,14 +902,13 @@ hipError_t wkv_launch_paged_attend(const WkvPagedCall& a, int dtype, int head_di
             // chunks onto 2000 slots of 32 heads on 8: 20 tokens 20.3 | 20.7 us, 40 23.1 | 22.2, 200 39.6 | 30.0.)
             const bool few = a.splits <= FEW, some = !few && a.splits <= SOME && rows >= MANY;
             const int sets = few || some ? THREADS * 4 / D : 1, joins = (rows + sets - 1) / sets;
-            const dim3 all((unsigned)(joins + units * per_unit));
-            if (few && a.starts) hipLaunchKernelGGL((wkv_paged_join_few_kernel<TT, D, FEW, false>), all, block, 0, stream, a, joins, rows, per_tile, 1);
-            else if (few) hipLaunchKernelGGL((wkv_paged_join_few_kernel<TT, D, FEW, true>), all, block, 0, stream, a, joins, rows, per_tile, per_unit);
-            else if (some && a.starts) hipLaunchKernelGGL((wkv_paged_join_few_kernel<TT, D, SOME, false>), all, block, 0, stream, a, joins, rows, per_tile, 1);
-            else if (some) hipLaunchKernelGGL((wkv_paged_join_few_kernel<TT, D, SOME, true>), all, block, 0, stream, a, joins, rows, per_tile, per_unit);
-            else if (a.starts) hipLaunchKernelGGL((wkv_paged_join_kernel<TT, D, false>), all, block, 0, stream, a, joins, per_tile, 1);
-            else hipLaunchKernelGGL((wkv_paged_join_kernel<TT, D, true>), all, block, 0, stream, a, joins, per_tile, per_unit);
-            e = hipGetLastError();
+            const unsigned all = (unsigned)(joins + units * per_unit);
+            if (few && a.starts) e = wkv_launch(&wkv_paged_join_few_kernel<TT, D, FEW, false>, all, THREADS, stream, a, joins, rows, per_tile, 1);
+            else if (few) e = wkv_launch(&wkv_paged_join_few_kernel<TT, D, FEW, true>, all, THREADS, stream, a, joins, rows, per_tile, per_unit);
+            else if (some && a.starts) e = wkv_launch(&wkv_paged_join_few_kernel<TT, D, SOME, false>, all, THREADS, stream, a, joins, rows, per_tile, 1);
+            else if (some) e = wkv_launch(&wkv_paged_join_few_kernel<TT, D, SOME, true>, all, THREADS, stream, a, joins, rows, per_tile, per_unit);
+            else if (a.starts) e = wkv_launch(&wkv_paged_join_kernel<TT, D, false>, all, THREADS, stream, a, joins, per_tile, 1);
+            else e = wkv_launch(&wkv_paged_join_kernel<TT, D, true>, all, THREADS, stream, a, joins, per_tile, per_unit);
         }
         return e;
     });
@@ -925,10 +923,11 @@ hipError_t wkv_launch_paged_sums(const WkvPagedCall& a, int dtype, int head_dim,
         constexpr int D = decltype(d)::value;
         for (int64_t u = 0; u < units;) {               // in pieces below 2^32 threads
             const int64_t n = std::min<int64_t>(units - u, ((1 << 24) - 1) / per_unit);
-            hipLaunchKernelGGL((wkv_paged_sums_kernel<TF32, D>), dim3((unsigned)(n * per_unit)), dim3(THREADS), 0, stream, a, (int)u, per_unit);
+            const hipError_t e = wkv_launch(&wkv_paged_sums_kernel<TF32, D>, (unsigned)(n * per_unit), THREADS, stream, a, (int)u, per_unit);
+            if (e != hipSuccess) return e;
             u += n;
         }
-        return hipGetLastError();
+        return hipSuccess;
     };
     return head_dim == 64 ? go(std::integral_constant<int, 64>{}) : go(std::integral_constant<int, 128>{});
 }
