@@ -89,3 +89,22 @@ def test_steps_and_short_chunks_keep_two_numbers_of_a_weight(dtype, d):
                 else:
                     p.v[p.where(b, j)] = x
         check(p, TWO, 0)
+
+
+def test_one_key_that_takes_nearly_all_in_a_large_launch():
+    """The kernel for long chunks with blocks of 32 keys, which launches of more than 512 workgroups take; the key in front of the chunk and within it,
+    where some of a tile's rows see it and others do not."""
+    lens, new = [420, 350, 400, 351, 410, 420], [350] * 6
+    for gap in (14.0, 20.0, 26.0):
+        for top in (0, 200):
+            p = Paged(83, lens, new, heads=32, kv_heads=32, d=128, page=64)
+            p.q[..., 0] = 4.0
+            p.q[..., 1:] *= 0.25
+            p.k[..., 0] = torch.where(torch.isnan(p.k[..., 0]), p.k[..., 0], 0.0)
+            p.k_new[..., 0] = 0.0
+            p.v, p.v_new = ((x * 500.0 + 1000.0).to(x.dtype) for x in (p.v, p.v_new))
+            for b, (n, m) in enumerate(zip(lens, new)):
+                for k, v, at in ((p.k_new, p.v_new, p.row(b, top - n + m)),) if top >= n - m else ((p.k, p.v, p.where(b, top)),):
+                    k[at], v[at] = 0.0, 0.0
+                    k[at][:, 0] = gap * math.sqrt(128) / 4.0
+            check(p, HALF_STEP["fp16"], 128)
