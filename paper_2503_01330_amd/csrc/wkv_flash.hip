@@ -23,6 +23,7 @@ namespace {
 
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
 
 constexpr int WAVES = 4, THREADS = 64 * WAVES, WAVE_ROWS = 32, TILE_ROWS = WAVES * WAVE_ROWS;
 
@@ -240,49 +241,21 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
 #pragma unroll
             for (int j = 0; j < 16; ++j) o[i][j] *= f;
     };
-    auto mask = [&](f32x16_t& s, int pos, int page0, int page1) __attribute__((always_inline)) {
+    // What rounding to fp16 takes from a weight below SMALL (a logit 18 and more below a row's largest) is up to 2^-25, and so a row's sum may miss the number
+    // of such weights times 2^-25 times the largest value.  (That matters where a key takes nearly all of a row and has a value near 0: the output is then
+    // left to such weights.)  Blocks that have some are counted, and their largest value is kept; if a row's sums are so small that the loss could be
+    // seen in them, the tile goes over its keys a second time, with the small weights by themselves.  4 x 4096 tokens: looking for small weights costs 5 %
+    // (612 -> 645 us), queries of 3 times the size, which have some in every block, 800 us (1170 with the small weights by themselves at once); a first key 22 above all others 867, with values of 0 1674.
+    [[maybe_unused]] int small_blocks = 0;
+    [[maybe_unused]] uint32_t largest = 0;                // two absolute values of fp16, as bits, which are in order
+    auto count_small = [&](uint32_t vb) __attribute__((always_inline)) {
+        ++small_blocks;
+#pragma unroll 2
+        for (int i = 0; i < BK * D / 512; ++i) {
+            const u32x4_t x = *lds_ptr<u32x4_t>(vb + lane * 16 + i * 1024);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            const int p = pos + (j >> 2) * 8 + half_q * 4 + (j & 3);
-            const int seen = ((j < 8 ? page0 : page1) >= 0) & (p <= p_row) & ((p > p_row - window) | (p < c.n_sink));
-            s[j] = seen ? s[j] : -INFINITY;
-        }
-    };
-    // What rounding to fp16 took from the block's weights below SMALL, by itself, raised by MORE: half a step of a weight is left of it down to 2^-55 of
-    // a row's largest, and 2^-66 of that one below.  (A key that takes nearly all of a row with a value near 0 leaves the output to such weights.)
-    // Wanted where a logit lies 18 or more below a row's largest.  Looking for that costs 3 to 5 % (4 x 4096 tokens 624 -> 658 us), a prompt that
-    // is full of such logits twice the time (6 times the queries: 1289 us).
-    auto small_weights = [&](uint32_t kb, uint32_t vb, int pos, const int (&pages)[NG], bool full) __attribute__((always_inline)) {
-        const float minus = ref == -INFINITY ? 0.f : -ref;
-#pragma unroll 1
-        for (int b = 0; b < NB; ++b) {
-            uint32_t k_from = k_at, v_from = v_at;        // (addresses and values for this are not kept in registers)
-            asm volatile("" : "+v"(k_from), "+v"(v_from));
-            f32x16_t s = logits(k_from, kb + b * 32 * (D * 2));
-            __builtin_amdgcn_sched_barrier(0);            // (one thing after the other, in few registers)
-            if (!full) mask(s, pos + b * 32, b ? pages[NG - 2] : pages[0], b ? pages[NG - 1] : pages[1]);
-            u32x4_t p[2];
-#pragma unroll
-            for (int w = 0; w < 8; ++w) {
-                float x[2], y[2];
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[w * 2 + e], a.scale, minus));
-                    x[e] = x[e] < SMALL ? x[e] : 0.f;
-                }
-                unpack2<TT>(pack2<TT>(x[0], x[1]), y[0], y[1]);
-                p[w >> 2][w & 3] = pack2<TT>((x[0] - y[0]) * MORE, (x[1] - y[1]) * MORE);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int i = 0; i < DB; ++i) {
-                f32x16_t d = {};
-#pragma unroll
-                for (int j = 0; j < 2; ++j) d = mfma32<TT>(values(v_from, vb + (b * 32 + j * 16) * (D * 2), i), p[j], d);
-#pragma unroll
-                for (int j = 0; j < 16; ++j) o[i][j] = __builtin_fmaf(d[j], 1.f / MORE, o[i][j]);
-                __builtin_amdgcn_sched_barrier(0);
-            }
+            for (int w = 0; w < 4; ++w)
+                largest = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2_t, largest), __builtin_bit_cast(u16x2_t, x[w] & 0x7FFF7FFFu)));
         }
     };
 
@@ -353,7 +326,7 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
         }
         if constexpr (NARROW) {
             asm volatile("" : "+v"(l));                   // (the weights have been added up: they are not kept for it)
-            if (__builtin_expect(full ? __any(least < SMALL) : edge, 0)) small_weights(kb, vb, pos, pages, full);
+            if (__builtin_expect(full ? __any(least < SMALL) : edge, 0)) count_small(vb);
         }
     };
 
@@ -365,30 +338,102 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
-    int pos = slot_of(begin), pages[NG], next = 0, after[NG];
-    if (begin < end) {
-        entries(pos, pages);
-        known(pos, pages);
-        load(s_k0, s_v0, pos, pages);
-        next = slot_of(min(begin + 1, end - 1));
-        entries(next, after);
-    }
-    auto round = [&](int blk, uint32_t k, uint32_t v, uint32_t k_next, uint32_t v_next) __attribute__((always_inline)) {
-        arrive();
-        known(next, after);
-        if (blk + 1 < end) load(k_next, v_next, next, after);
-        const int p = pos;
-        int e[NG];
+    auto sweep = [&](auto&& use) __attribute__((always_inline)) {
+        int pos = slot_of(begin), pages[NG], next = 0, after[NG];
+        if (begin < end) {
+            entries(pos, pages);
+            known(pos, pages);
+            load(s_k0, s_v0, pos, pages);
+            next = slot_of(min(begin + 1, end - 1));
+            entries(next, after);
+        }
+        auto round = [&](int blk, uint32_t k, uint32_t v, uint32_t k_next, uint32_t v_next) __attribute__((always_inline)) {
+            arrive();
+            known(next, after);
+            if (blk + 1 < end) load(k_next, v_next, next, after);
+            const int p = pos;
+            int e[NG];
 #pragma unroll
-        for (int i = 0; i < NG; ++i) { e[i] = pages[i]; pages[i] = after[i]; }
-        pos = next;
-        next = slot_of(min(blk + 2, end - 1));
-        entries(next, after);
-        use(k, v, p, e);
+            for (int i = 0; i < NG; ++i) { e[i] = pages[i]; pages[i] = after[i]; }
+            pos = next;
+            next = slot_of(min(blk + 2, end - 1));
+            entries(next, after);
+            use(k, v, p, e);
+        };
+        for (int blk = begin; blk < end; blk += 2) {
+            round(blk, s_k0, s_v0, s_k1, s_v1);
+            if (blk + 1 < end) round(blk + 1, s_k1, s_v1, s_k0, s_v0);
+        }
     };
-    for (int blk = begin; blk < end; blk += 2) {
-        round(blk, s_k0, s_v0, s_k1, s_v1);
-        if (blk + 1 < end) round(blk + 1, s_k1, s_v1, s_k0, s_v0);
+    sweep(use);
+    l = pair_sum<32>(l);
+
+    if constexpr (NARROW) {
+        bool again = false;
+        if (small_blocks > 0) {
+            uint32_t v = max(largest & 0xFFFF, largest >> 16);
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) v = max(v, (uint32_t)__shfl_xor((int)v, d));
+            const float lost = (float)(small_blocks * BK) * 0x1p-25f * (float)__builtin_bit_cast(_Float16, (uint16_t)v);
+            float top = 0.f, x0, x1;
+#pragma unroll
+            for (int i = 0; i < DB; ++i)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) top = fmaxf(top, __builtin_fabsf(o[i][j]));
+            lane_pair<32>(top, x0, x1);
+            top = fmaxf(x0, x1);
+            // half of fp16's smallest step, or a 64th of half a step of the row's largest output
+            again = __any(l > 0.f && lost > l * 0x1p-25f && lost > top * 0x1p-18f);
+        }
+        if (__builtin_expect(__syncthreads_or(again), 0)) {
+            // The reference stays as it is now.  What rounding takes from a weight below SMALL goes by itself, raised by MORE: half a step of a weight is left
+            // of it down to 2^-55 of a row's largest, and 2^-66 of that one below.
+#pragma unroll
+            for (int i = 0; i < DB; ++i)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
+            const float minus = ref == -INFINITY ? 0.f : -ref;
+            sweep([&](uint32_t kb, uint32_t vb, int pos, const int (&pages)[NG]) __attribute__((always_inline)) {
+                if (pos > p_hi) return;
+#pragma unroll 1
+                for (int b = 0; b < NB; ++b) {
+                    uint32_t k_from = k_at, v_from = v_at;
+                    asm volatile("" : "+v"(k_from), "+v"(v_from));        // (addresses made of these are not kept in registers)
+                    f32x16_t s = logits(k_from, kb + b * 32 * (D * 2));
+                    __builtin_amdgcn_sched_barrier(0);    // (one thing after the other, in few registers)
+                    u32x4_t p[2], more[2];
+#pragma unroll
+                    for (int w = 0; w < 8; ++w) {
+                        const int page = b ? pages[NG - 2 + (w >> 2)] : pages[w >> 2];
+                        float x[2], y[2];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const int j = 2 * w + e, at = pos + b * 32 + (j >> 2) * 8 + half_q * 4 + (j & 3);
+                            const int seen = (page >= 0) & (at <= p_row) & ((at > p_row - window) | (at < c.n_sink));
+                            x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j], a.scale, minus));
+                            x[e] = seen ? x[e] : 0.f;
+                        }
+                        p[w >> 2][w & 3] = pack2<TT>(x[0], x[1]);
+                        unpack2<TT>(p[w >> 2][w & 3], y[0], y[1]);
+                        more[w >> 2][w & 3] = pack2<TT>(x[0] < SMALL ? (x[0] - y[0]) * MORE : 0.f, x[1] < SMALL ? (x[1] - y[1]) * MORE : 0.f);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+#pragma unroll
+                    for (int i = 0; i < DB; ++i) {
+                        f32x16_t d = {};
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const u32x4_t v = values(v_from, vb + (b * 32 + j * 16) * (D * 2), i);
+                            o[i] = mfma32<TT>(v, p[j], o[i]);
+                            d = mfma32<TT>(v, more[j], d);
+                        }
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) o[i][j] = __builtin_fmaf(d[j], 1.f / MORE, o[i][j]);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+            });
+        }
     }
 
     // (the lane's row once more, so that it takes no registers in the loop above)
@@ -396,7 +441,6 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
     asm("" : "+v"(tid));
     const int row = w0 + (tid & 31), token = min(row, r1 - 1) / group, head = t.h * group + min(row, r1 - 1) - token * group, half = tid >> 5 & 1;
 
-    l = pair_sum<32>(l);
     // A value that is not finite spoils the sums of rows that do not see it (0 x infinity), and sums of the largest values may overflow.  If one is
     // not finite, the wave forms them anew, key by key: a lane has a row and half of its elements.
     float z = 0.f;

@@ -108,3 +108,25 @@ def test_one_key_that_takes_nearly_all_in_a_large_launch():
                     k[at], v[at] = 0.0, 0.0
                     k[at][:, 0] = gap * math.sqrt(128) / 4.0
             check(p, HALF_STEP["fp16"], 128)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_one_key_with_values_of_0_in_some_elements(d):
+    """Where a row's largest output is not small, what the long chunks' kernel may lose of the others is below a 64th of half a step of that."""
+    for gap in (18.0, 24.0, 30.0):
+        p = Paged(84, [1500, 130], [300, 60], heads=8, kv_heads=2, d=d, page=64)
+        p.q[..., 0] = 4.0
+        p.q[..., 1:] *= 0.25
+        p.k[..., 0] = torch.where(torch.isnan(p.k[..., 0]), p.k[..., 0], 0.0)
+        p.k_new[..., 0] = 0.0
+        p.v, p.v_new = ((x * 500.0 + 1000.0).to(x.dtype) for x in (p.v, p.v_new))
+        for b in (0, 1):
+            at = p.where(b, 7)
+            p.k[at] = 0.0
+            p.k[at][:, 0] = gap * math.sqrt(d) / 4.0
+            p.v[at][:, ::2] = 0.0
+        x = p.device()
+        x["cache"].prefill(x["q"], x["k_new"], x["v_new"], x["out"], x["starts"], 300)
+        torch.cuda.synchronize()
+        out, tol = attend(p, HALF_STEP["fp16"], d)
+        paged.close(x["out"], out, tol + 2.0 ** -18 * out.abs().amax(-1, keepdim=True), "out")
