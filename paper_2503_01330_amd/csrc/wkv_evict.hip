@@ -6,10 +6,10 @@
 //                     reading a stretch before it writes it, overwrites nothing that is still needed; workgroups share out K, V
 //                     and pieces of the rows, which do not touch each other.  The sums move the same way.
 //
-// 4 x 32768 slots of 8 heads of 128 to 2048, fp16: select 24.8 us (a unit's scores on one compute unit, in registers: three counts by LDS atomics,
-// four barriers each, and the list; 4 MB of scores would take 1), move 14.2 us for 37 MB read and 38 MB written, by 288 workgroups, each once
+// 4 x 32768 slots of 8 heads of 128 to 2048, fp16: select 23.6 us (a unit's scores on one compute unit, in registers: three counts by LDS atomics,
+// four barriers each, and the list; 4 MB of scores would take 1), move 13.8 us for 37 MB read and 38 MB written, by 288 workgroups, each once
 // through the chain list, rows, writes.
-// 5 x up to 1237 slots of 12 heads of 64 to 255: 9.0 + 4.4 us.
+// 5 x up to 1237 slots of 12 heads of 64 to 255: 9.0 + 4.3 us.
 #include "../../include/wkv.h"
 #include "wkv_internal.h"
 #include "wkv_device.h"

@@ -7,9 +7,10 @@
 // of one element, is read from LDS transposed.  A softmax with a running reference: the sums are scaled down only where a logit
 // exceeds the reference by more than 8 octaves (fp16: 15, with a reference 12 below the logit that sets it).
 //
-// Bound by the matrix and the vector instructions (exponentials, maxima, conversions of the logits), and by the clock, which falls to 1.7 GHz as
-// both fill: 4 x 4096 tokens, 32 heads on 8 of 128, fp16: 622 us, 883 TFLOP/s, the matrix units busy 51 % of the cycles, LDS 26 %, none of these
-// waiting for a bank; window 1024 over 2 x 8192 327 us.  What is read once comes from memory 1.2 times (234 MB of 201).
+// Bound by the matrix and the vector instructions (exponentials, maxima, conversions of the logits), and by the clock, which falls to 1.8 GHz as
+// both fill: 4 x 4096 tokens, 32 heads on 8 of 128, fp16: 645 us, 852 TFLOP/s, the matrix units busy 45 % of the cycles, LDS 23 %, none of these
+// waiting for a bank; bf16, which does not look for small weights, 575 us; window 1024 over 2 x 8192, bf16, 320 us.  What is read once comes from memory
+// 1.2 times (233 MB of 201).
 // (A first kernel of 16 rows a workgroup took 2679 us.)
 #include "../../include/wkv.h"
 #include "wkv_internal.h"
@@ -70,8 +71,9 @@ template <int D, int KEYS> struct Block {
     static constexpr int turn_v(int key) { return D == 64 ? (key >> 1 & 1) << 2 : (key & 3) << 2; }
 };
 
-// BK: keys of a block, 64 or 32.  With 32 and rows of 256 bytes three workgroups share a compute unit (167 registers, 32 KB), with 64 two (222): the
-// first is ahead where there are that many (4 x 4096 646 -> 622 us, window 1024 over 2 x 8192 373 -> 336), the other where not (2048 tokens 82 | 70).
+// BK: keys of a block, 64 or 32.  With 32 and rows of 256 bytes three workgroups share a compute unit (167 registers, 32 KB), with 64 two (207 to 222): the
+// first is ahead where there are that many (us with 64 | 32, bf16: 4 x 4096 tokens 582 | 564, window 1024 over 2 x 8192 366 | 313; fp16 636 | 634, 395 | 348),
+// the other where not (2048 tokens, bf16 60 | 70, fp16 66 | 80).
 template <class TT, int D, int BK>
 __global__ __launch_bounds__(THREADS, D * BK > 4096 ? 2 : 3)
 void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)

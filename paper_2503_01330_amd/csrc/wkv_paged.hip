@@ -16,9 +16,9 @@
 //
 // Softmax statistics, sums of the weights and of weight . v are fp32.
 //
-// Long steps are bound by memory: 4 x 32768 slots, 32 heads on 8 of 128, fp16: wkv_paged_rows 88.7 us for 537 MB of K and V (6.05 TB/s; 547 MB
-// fetched), the join 4.8.  64 ragged sequences of up to 4096 with logits 131 us for 565 + 19 MB, join and tally 13.3.  Short ones by the chain
-// launch, table, rows, joins: 4096 slots of one sequence 6.3 + 4.0 us, 64 slots in fp32 4.9.  (Waves that keep K and V in registers, one block
+// Long steps are bound by memory: 4 x 32768 slots, 32 heads on 8 of 128, fp16: wkv_paged_rows 88.5 us for 537 MB of K and V (6.07 TB/s; 547 MB
+// fetched), the join 4.8.  64 ragged sequences of up to 4096 with logits 131 us for 565 + 19 MB, join and tally 13.5.  Short ones by the chain
+// launch, table, rows, joins: 4096 slots of one sequence 6.1 + 3.9 us, 64 slots in fp32 4.7.  (Waves that keep K and V in registers, one block
 // ahead, and no LDS but for the joins: a first kernel that staged a block at a time took 117 us for the long step, 28 for the one sequence.)
 #include "../../include/wkv.h"
 #include "wkv_internal.h"
@@ -846,7 +846,7 @@ void wkv_paged_shape(WkvPagedCall& a, int64_t units, int64_t rows, int64_t most,
     auto over = [&](int64_t n) { return (n + groups - 1) / groups; };
     auto parts = [&](int64_t want, int64_t least) { return (int)std::max<int64_t>(1, std::min<int64_t>({want, (most + least - 1) / least, 64})); };
     // Chunks of different lengths: room for the tiles that n_tokens can have, where as many as the longest chunk has for every sequence are several times
-    // that.  us with a workgroup for each of those | packed: 64 chunks of 128 tokens and one of 512 (3 times) 136 | 138, of 128 and 1024 (6) 148 | 155,
+    // that.  us with a workgroup for each of these | packed: 64 chunks of 128 tokens and one of 512 (3 times) 136 | 138, of 128 and 1024 (6) 148 | 155,
     // 200 of 64 and 1024 (10) 109 | 100, 64 of 64 and 2048 (16) 165 | 139, 256 of 4 and 8192 (121) 1104 | 670; the other kernel, fp32, 128 of 64 and 512
     // (3) 104 | 84, of 16 and 1024 (7) 132 | 56.
     a.slots = 0;
