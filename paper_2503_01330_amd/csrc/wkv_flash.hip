@@ -247,7 +247,8 @@ void wkv_paged_flash_kernel(const WkvPagedCall a, int tiles, int spread)
     // of such weights times 2^-25 times the largest value.  (That matters where a key takes nearly all of a row and has a value near 0: the output is then
     // left to such weights.)  Blocks that have some are counted, and their largest value is kept; if a row's sums are so small that the loss could be
     // seen in them, the tile goes over its keys a second time, with the small weights by themselves.  4 x 4096 tokens: looking for small weights costs 5 %
-    // (612 -> 645 us), queries of 3 times the size, which have some in every block, 800 us (1170 with the small weights by themselves at once); a first key 22 above all others 867, with values of 0 1674.
+    // (612 -> 645 us), queries of 3 times the size, which have some in every block, 800 us (1170 with the small weights by themselves at once); a first
+    // key 22 above all others 867, with values of 0 1674.
     [[maybe_unused]] int small_blocks = 0;
     [[maybe_unused]] uint32_t largest = 0;                // two absolute values of fp16, as bits, which are in order
     auto count_small = [&](uint32_t vb) __attribute__((always_inline)) {

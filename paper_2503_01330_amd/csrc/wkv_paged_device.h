@@ -45,10 +45,11 @@ template <class TT> __device__ __forceinline__ void unpack2(uint32_t w, float& l
     }
 }
 
-// Weights are 2^(logit - reference), the reference being a logit (log2) that none exceeds by more than 8 (fp16: a number that none exceeds by more than 15), so sums of 16-bit values up to 2^128 and of
-// fp32 values may leave the range of fp32 although their mean does not.  Such a sum is formed anew with every weight times
-// 2^-CAREFUL, which is a larger reference (a sequence has at most 2^24 slots); a reference that is larger from the start would cost the exponents
-// of all weights 5 bits.  Where sums of several waves or parts are joined, the common reference is JOINED above the largest.
+// Weights are 2^(logit - reference), the reference being a logit (log2) that none exceeds by more than 8 (fp16: a number that none exceeds by
+// more than 15), so sums of 16-bit values up to 2^128 and of fp32 values may leave the range of fp32 although their mean does not.  Such a sum is
+// formed anew with every weight times 2^-CAREFUL, which is a larger reference (a sequence has at most 2^24 slots); a reference that is larger from
+// the start would cost the exponents of all weights 5 bits.  Where sums of several waves or parts are joined, the common reference is JOINED above
+// the largest.
 template <class TT> constexpr float CAREFUL = __is_same(TT, TF16) ? 0.f : 32.f;
 constexpr float JOINED = 8.f;
 
